@@ -432,6 +432,128 @@ const char *palq_net_layer_kernels(const palq_net *net, int32_t layer, int32_t i
 palq_status palq_net_layer_times(palq_net *net, float *ms, int32_t *forwards);
 palq_status palq_net_reset_times(palq_net *net);
 
+/* ------------------------------------------- 8-bit transformer operators
+ *
+ * The products and the attention of a transformer whose weights,
+ * activations and key/value cache are 8-bit codes: what a language or vision
+ * model served beside the convolutional networks above needs.  Floating
+ * tensors are fp32, fp16 or bf16; codes are int8 with fp32 scales.
+ *
+ * Quantiser of these operators, in fp32 arithmetic, over a row (one token) or
+ * a block (the tokens of one cache page, one head):
+ *   a = max |x|;  s = max(a * fl(1/127), 2^-100);
+ *   code = clamp(rint(x * fl(1/s)), -127, 127), ties to even.
+ * A row or block with an element that is not finite has scale NaN and its
+ * codes are 0, so the results that depend on it, and no others, are NaN.
+ */
+#define PALQ_F32 0
+#define PALQ_F16 1
+#define PALQ_BF16 2
+#define PALQ_I8 3 /* codes, with their scales in an argument of their own */
+
+/* Token quantiser: codes[r][0..cols) and scales[r] of each of `rows` rows of
+ * x (type PALQ_F32, F16 or BF16; rows x_ld elements apart, codes codes_ld
+ * bytes apart).  Pointers aligned to their elements; rows and pointers that
+ * are multiples of 16 bytes apart run faster.  x, codes and scales must not
+ * overlap. */
+palq_status palq_quantize_rows(palq_ctx *ctx, const void *x, int32_t type, int64_t rows, int32_t cols, int64_t x_ld,
+                               int8_t *codes, int64_t codes_ld, float *scales);
+
+/* Weights of y = x W^T + bias laid out for the matrix cores, once. */
+typedef struct palq_linear palq_linear;
+
+/* w: int8 codes [n_out] rows of n_in, w_ld bytes apart, w_scale fp32 [n_out],
+ * bias fp32 [n_out] or NULL; all device, copied (the caller may free them
+ * once this returns; it synchronises the context's stream).  Runs of up to
+ * max_rows rows need no further memory: the workspace for them (shared by all
+ * products and attention calls of the context) is reserved here.
+ * PALQ_ERR_OVERFLOW when n_in >= 2^17 (the int32 sum of products could
+ * overflow); PALQ_ERR_NOMEM.  A validate-only context returns a layer that
+ * runs nothing. */
+palq_status palq_linear_create(palq_ctx *ctx, const int8_t *w, int64_t w_ld, const float *w_scale, const float *bias,
+                               int32_t n_out, int32_t n_in, int64_t max_rows, palq_linear **out);
+/* y[m][n] = (sum_k c[m][k] w[n][k]) * s[m] * w_scale[n] + bias[n], the sum
+ * exact in int32, the rest in fp32, one rounding to y_type.  x_type PALQ_F32,
+ * F16 or BF16: c, s are x's rows through the quantiser above (x_scale NULL);
+ * PALQ_I8: x holds c and x_scale (device, fp32 [rows]) s.  Rows of x and y
+ * are x_ld and y_ld elements apart.  Enqueues kernels only (no allocation, no
+ * synchronisation): may be captured into a graph, which holds the layer's
+ * and the context's memory.  PALQ_ERR_ARG: rows > max_rows, a layer of
+ * another context, misaligned or overlapping (address ranges of) x and y. */
+palq_status palq_linear_run(palq_ctx *ctx, const palq_linear *lin, const void *x, int32_t x_type, int64_t x_ld,
+                            const float *x_scale, int64_t rows, void *y, int32_t y_type, int64_t y_ld);
+/* Frees a layer (waits for device work that still reads it). */
+void palq_linear_destroy(palq_linear *lin);
+/* The kernel a run of `rows` rows takes (static host string; "" for a
+ * validate-only layer, NULL for a null one). */
+const char *palq_linear_kernels(const palq_linear *lin, int64_t rows);
+
+/* A paged key/value cache of one layer.  A page holds page_tokens (16, 32, 64
+ * or 128) tokens of every head, head_dim 64, 96, 128 or 256:
+ *   k int8 [pages][heads][page_tokens][head_dim]
+ *   v int8 [pages][heads][head_dim][page_tokens]   (channel by channel)
+ *   k_scale, v_scale fp32 [pages][heads]: one scale for each block
+ * all device, owned by the caller, k and v 16-byte aligned. */
+typedef struct {
+  int32_t pages, page_tokens, heads, head_dim;
+  int8_t *k, *v;
+  float *k_scale, *v_scale;
+} palq_cache;
+
+/* A batch of requests of different lengths (device arrays, host sizes).
+ * Request r's token j lies on page table[r][j / page_tokens], place
+ * j % page_tokens; it has lens[r] tokens.  Rows starts[r] .. starts[r + 1] of
+ * the tensors of a call (`tokens` rows in all) are its LAST positions,
+ * lens[r] - (starts[r + 1] - starts[r]) and on: for an append or the attention
+ * of the same step, lens counts the new tokens.
+ *   table int32 [requests][max_pages], lens int32 [requests],
+ *   starts int32 [requests + 1]
+ *   max_new: at least every request's rows; max_len: at least every lens[r]
+ *   (they size the launches; closer bounds run faster).
+ * Device values outside these bounds never lead outside the tensors: rows
+ * past max_new and tokens past max_len or the table are left out, as are
+ * tokens on a page number outside [0, pages). */
+typedef struct {
+  int32_t requests, max_pages;
+  const int32_t *table, *lens, *starts;
+  int64_t tokens;
+  int32_t max_new, max_len;
+} palq_batch;
+
+/* Quantises the new keys and values of a batch into their pages: k, v of
+ * `type`, [tokens][heads][head_dim] with rows k_row / v_row and heads k_head /
+ * v_head elements apart (a head's channels are consecutive).  In a block that
+ * already holds tokens the scale becomes the larger of its own and the new
+ * tokens'; where it grew, old codes are rescaled to
+ * rint(code * fl(s_old / s)).  A block whose first token is new starts
+ * afresh, whatever its page held.  Pages of different requests must be
+ * distinct where they are written.  Appending the same values again leaves
+ * the cache as it is. */
+palq_status palq_cache_append(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *k, int64_t k_row,
+                              int64_t k_head, const void *v, int64_t v_row, int64_t v_head, int32_t type);
+/* The inverse: code * scale of each request's last tokens, to tensors laid
+ * out as in palq_cache_append; 0 for tokens on pages out of range. */
+palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, void *k, int64_t k_row,
+                            int64_t k_head, void *v, int64_t v_row, int64_t v_head, int32_t type);
+
+/* Attention of a batch's rows over its cached tokens.  q, out: PALQ_F16 or
+ * PALQ_BF16 [tokens][q_heads][head_dim], strides in elements as above;
+ * q_heads a multiple of cache->heads, query head i reads cache head
+ * i / (q_heads / heads).
+ *   out = sum_j p_j v_j,  p = softmax_j(scale * q . k_j)
+ * over the tokens j < lens[r] that a row sees: with causal = 1 those up to its
+ * own position, with window > 0 only the last `window` of them; with
+ * causal = 0 all (cross attention to cached encoder states: the rows then
+ * have no position, and may outnumber the tokens).  A row that sees no token
+ * gives 0.  Scores, softmax and sums are fp32; probabilities enter the second
+ * product in fp16.  Long caches of few rows are split and joined in the
+ * context's workspace, which may grow (never while a graph is captured:
+ * PALQ_ERR_NOMEM then; run the shape once before).  out and q (address ranges)
+ * must not overlap. */
+palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *q, int64_t q_row,
+                           int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head, int32_t type,
+                           float scale, int32_t causal, int32_t window);
+
 #ifdef __cplusplus
 }
 #endif

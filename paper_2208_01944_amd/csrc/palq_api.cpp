@@ -120,6 +120,7 @@ palq_status palq_create(int32_t device, void *hip_stream, palq_ctx **out) {
     if (e == hipSuccess) noalloc_scratch_init(device);
     if (e == hipSuccess) e = hipMalloc(&ctx->range_scratch, range_parts_bytes());
     if (e == hipSuccess) e = hipEventCreateWithFlags(&ctx->order_event, hipEventDisableTiming);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&ctx->cus, hipDeviceAttributeMultiprocessorCount, device);
     if (e != hipSuccess) {
       if (ctx->range_scratch) hipFree(ctx->range_scratch);
       delete ctx;
@@ -139,6 +140,7 @@ void palq_destroy(palq_ctx *ctx) {
     if (ctx->fc_scratch) hipFree(ctx->fc_scratch);
     if (ctx->mod_scratch) hipFree(ctx->mod_scratch);
     if (ctx->order_event) hipEventDestroy(ctx->order_event);
+    for (uint8_t *w : ctx->work) hipFree(w);
   }
   delete ctx;
 }

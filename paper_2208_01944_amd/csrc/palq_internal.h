@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <string>
+#include <vector>
 
 #include "palq.h"
 
@@ -248,6 +249,11 @@ struct palq_ctx {
   uint8_t *mod_scratch = nullptr;  // rotated parameters of the last shuffle-module call
   size_t mod_scratch_bytes = 0;
   hipEvent_t order_event = nullptr;  // palq_set_stream: the new stream waits for the old one
+  // workspace of the transformer operators: the newest of `work` is in use, the
+  // smaller ones before it stay for graphs that captured them
+  std::vector<uint8_t *> work;
+  size_t work_bytes = 0;
+  int cus = 0;                       // compute units (0: validate only)
 };
 
 // A planned single layer (palq_conv_plan_create / palq_conv_run).

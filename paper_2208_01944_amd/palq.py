@@ -32,6 +32,8 @@ OK, ERR_ARG, ERR_UNSUPPORTED, ERR_OVERFLOW, ERR_DEVICE, ERR_NOMEM = 0, -1, -2, -
 OP_CONV, OP_MAXPOOL, OP_AVGSUM, OP_FC, OP_SHUFFLE_MODULE, OP_CHANNEL_SHUFFLE = 1, 2, 3, 4, 5, 6
 NET_KEEP_ALL, NET_TIMING, NET_GRAPH, NET_PIXEL_LAYOUT = 1, 2, 4, 8
 LAYOUT_PIXEL, LAYOUT_GROUP = 0, 1
+F32, F16, BF16, I8 = 0, 1, 2, 3  # element types of the transformer operators
+_TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
 
 
 class Act(ctypes.Structure):
@@ -62,6 +64,16 @@ class Layer(ctypes.Structure):
                 ("proj_src", c_i32), ("proj_w", Filter), ("proj_stride", c_i32),
                 ("pool_k", c_i32), ("pool_stride", c_i32), ("pool_pad", c_i32), ("fc_w", c_p),
                 ("fc_out", c_i32)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("pages", c_i32), ("page_tokens", c_i32), ("heads", c_i32), ("head_dim", c_i32),
+                ("k", c_p), ("v", c_p), ("k_scale", c_p), ("v_scale", c_p)]
+
+
+class BatchDesc(ctypes.Structure):
+    _fields_ = [("requests", c_i32), ("max_pages", c_i32), ("table", c_p), ("lens", c_p), ("starts", c_p),
+                ("tokens", c_i64), ("max_new", c_i32), ("max_len", c_i32)]
 
 
 def _sig(name, res, *args):
@@ -111,6 +123,16 @@ _net_ops = _sig("palq_net_ops", c_i64, c_p)
 _net_layer_kernels = _sig("palq_net_layer_kernels", ctypes.c_char_p, c_p, c_i32, c_i32)
 _net_layer_times = _sig("palq_net_layer_times", c_i32, c_p, ctypes.POINTER(c_f), ctypes.POINTER(c_i32))
 _net_reset_times = _sig("palq_net_reset_times", c_i32, c_p)
+_quantize_rows = _sig("palq_quantize_rows", c_i32, c_p, c_p, c_i32, c_i64, c_i32, c_i64, c_p, c_i64, c_p)
+_linear_create = _sig("palq_linear_create", c_i32, c_p, c_p, c_i64, c_p, c_p, c_i32, c_i32, c_i64, ctypes.POINTER(c_p))
+_linear_run = _sig("palq_linear_run", c_i32, c_p, c_p, c_p, c_i32, c_i64, c_p, c_i64, c_p, c_i32, c_i64)
+_linear_destroy = _sig("palq_linear_destroy", None, c_p)
+_linear_kernels = _sig("palq_linear_kernels", ctypes.c_char_p, c_p, c_i64)
+P_CACHE, P_BATCH = ctypes.POINTER(CacheDesc), ctypes.POINTER(BatchDesc)
+_cache_append = _sig("palq_cache_append", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_p, c_i64, c_i64, c_i32)
+_cache_read = _sig("palq_cache_read", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_p, c_i64, c_i64, c_i32)
+_attention = _sig("palq_attention", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_f,
+                  c_i32, c_i32)
 
 EXPORTS = ["palq_create", "palq_destroy", "palq_set_stream", "palq_set_conv_fp4", "palq_set_conv_bitdecomp", "palq_sync", "palq_last_error",
            "palq_version", "palq_row_bytes", "palq_act_bytes", "palq_pack", "palq_unpack",
@@ -119,7 +141,8 @@ EXPORTS = ["palq_create", "palq_destroy", "palq_set_stream", "palq_set_conv_fp4"
            "palq_channel_shuffle", "palq_maxpool",
            "palq_avgsum", "palq_fc", "palq_net_create", "palq_net_destroy", "palq_forward",
            "palq_forward_image", "palq_net_tensor", "palq_net_ops", "palq_net_layer_kernels", "palq_net_layer_times",
-           "palq_net_reset_times"]
+           "palq_net_reset_times", "palq_quantize_rows", "palq_linear_create", "palq_linear_run", "palq_linear_destroy",
+           "palq_linear_kernels", "palq_cache_append", "palq_cache_read", "palq_attention"]
 
 
 class PalqError(RuntimeError):
@@ -295,6 +318,155 @@ class Context:
 
     def fc(self, x, n, cin, w, cout, logits):
         self._check(_fc(self.h, _ptr(x), n, cin, _ptr(w), cout, _ptr(logits)))
+
+    # ----------------------------------------------------------- 8-bit transformer operators
+    def quantize_rows(self, x, codes, scales):
+        """palq_quantize_rows: x [rows, cols] floating -> codes int8 [rows, cols], scales fp32 [rows]."""
+        if codes.dtype != torch.int8 or tuple(codes.shape) != tuple(x.shape):
+            raise PalqError(ERR_ARG, "codes must be int8 of x's shape")
+        _need(scales, torch.float32, x.shape[0], "scales")
+        xt, x_ld = _rows2(x)
+        _, c_ld = _rows2(codes)
+        self._check(_quantize_rows(self.h, x.data_ptr(), xt, x.shape[0], x.shape[1], x_ld, codes.data_ptr(), c_ld,
+                                   scales.data_ptr()))
+
+    def cache_append(self, cache: Cache, k, v, batch: Batch):
+        """palq_cache_append: k, v [tokens, heads, head_dim] into the pages of their requests."""
+        kt, kr, kh = _rows3(k, batch, cache)
+        vt, vr, vh = _rows3(v, batch, cache)
+        if kt != vt or k.shape != v.shape:
+            raise PalqError(ERR_ARG, "k and v differ in type or shape")
+        self._check(_cache_append(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, kt))
+
+    def cache_read(self, cache: Cache, k, v, batch: Batch):
+        """palq_cache_read: the values of each request's last tokens into k, v [tokens, heads, head_dim]."""
+        kt, kr, kh = _rows3(k, batch, cache)
+        vt, vr, vh = _rows3(v, batch, cache)
+        if kt != vt or k.shape != v.shape:
+            raise PalqError(ERR_ARG, "k and v differ in type or shape")
+        self._check(_cache_read(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, kt))
+
+    def attention(self, cache: Cache, q, out, batch: Batch, scale, causal=True, window=0):
+        """palq_attention: q, out [tokens, q_heads, head_dim]."""
+        qt, qr, qh = _rows3(q, batch, cache, cache.q_heads_ok)
+        ot, orow, oh = _rows3(out, batch, cache, cache.q_heads_ok)
+        if qt != ot or q.shape != out.shape:
+            raise PalqError(ERR_ARG, "q and out differ in type or shape")
+        self._check(_attention(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, qt,
+                               scale, causal, window))
+
+
+class Linear:
+    """Weights of an 8-bit product with scales for each token and channel
+    (palq_linear_create): w int8 [n_out, n_in], w_scale fp32 [n_out], bias
+    fp32 [n_out] or None; copied."""
+
+    def __init__(self, ctx: Context, w, w_scale, bias=None, max_rows=0):
+        if w.dtype != torch.int8:
+            raise PalqError(ERR_ARG, "w must be int8")
+        self.ctx, (self.n_out, self.n_in) = ctx, w.shape
+        _need(w_scale, torch.float32, self.n_out, "w_scale")
+        if bias is not None:
+            _need(bias, torch.float32, self.n_out, "bias")
+        _, w_ld = _rows2(w)
+        h = c_p()
+        ctx._check(_linear_create(ctx.h, w.data_ptr(), w_ld, w_scale.data_ptr(), _ptr(bias), self.n_out, self.n_in, max_rows,
+                                  ctypes.byref(h)))
+        self.h = h
+
+    def kernels(self, rows) -> str:
+        return _linear_kernels(self.h, rows).decode()
+
+    def run(self, x, y, x_scale=None):
+        """y [rows, n_out] from x [rows, n_in]: floating values, or int8 codes with x_scale fp32 [rows]."""
+        xt, x_ld = _rows2(x)
+        yt, y_ld = _rows2(y)
+        rows = x.shape[0]
+        if x.shape[1] != self.n_in or y.shape[0] != rows or y.shape[1] != self.n_out:
+            raise PalqError(ERR_ARG, "x or y does not have the layer's shape")
+        if x_scale is not None:
+            _need(x_scale, torch.float32, rows, "x_scale")
+            x_scale = x_scale.data_ptr()
+        self.ctx._check(_linear_run(self.ctx.h, self.h, x.data_ptr(), xt, x_ld, x_scale, rows, y.data_ptr(), yt, y_ld))
+
+    def __del__(self):
+        h = getattr(self, "h", None)
+        if h:
+            _linear_destroy(h)
+            self.h = None
+
+
+class Cache:
+    """A paged 8-bit key/value cache (palq_cache) over tensors of the caller:
+    k int8 [pages, heads, page_tokens, head_dim], v int8 [pages, heads,
+    head_dim, page_tokens], k_scale and v_scale fp32 [pages, heads]."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        pages, heads, page, dim = k.shape
+        if tuple(v.shape) != (pages, heads, dim, page) or k.dtype != torch.int8 or v.dtype != torch.int8:
+            raise PalqError(ERR_ARG, "k and v must be int8 [pages, heads, page, dim] and [pages, heads, dim, page]")
+        if not k.is_contiguous() or not v.is_contiguous():
+            raise PalqError(ERR_ARG, "k and v must be contiguous")
+        _need(k_scale, torch.float32, pages * heads, "k_scale")
+        _need(v_scale, torch.float32, pages * heads, "v_scale")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.heads, self.page, self.dim = pages, heads, page, dim
+        self.desc = CacheDesc(pages, page, heads, dim, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+    @staticmethod
+    def empty(pages, heads, page, dim, device="cuda"):
+        """A cache on memory of its own; every code 0."""
+        return Cache(torch.zeros(pages, heads, page, dim, dtype=torch.int8, device=device),
+                     torch.zeros(pages, heads, dim, page, dtype=torch.int8, device=device),
+                     torch.ones(pages, heads, device=device), torch.ones(pages, heads, device=device))
+
+    def q_heads_ok(self, n):
+        return n % self.heads == 0
+
+
+class Batch:
+    """A batch of requests (palq_batch): table int32 [requests, max_pages],
+    lens int32 [requests], starts int32 [requests + 1] on the device, and the
+    host's bounds for rows and tokens of one request."""
+
+    def __init__(self, table, lens, starts, max_new, max_len):
+        requests, max_pages = table.shape
+        if table.dtype != torch.int32 or not table.is_contiguous():
+            raise PalqError(ERR_ARG, "table must be contiguous int32")
+        _need(lens, torch.int32, requests, "lens")
+        _need(starts, torch.int32, requests + 1, "starts")
+        self.table, self.lens, self.starts = table, lens, starts
+        self.desc = BatchDesc(requests, max_pages, table.data_ptr(), lens.data_ptr(), starts.data_ptr(), 0, max_new, max_len)
+        self.ref = ctypes.byref(self.desc)
+
+
+def _need(t, dtype, n, what):
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise PalqError(ERR_ARG, f"{what} must be {n} contiguous values of {dtype}")
+
+
+def _rows2(t):
+    """Type and row stride of a [rows, cols] tensor with consecutive columns."""
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise PalqError(ERR_ARG, "a row's elements must be consecutive")
+    if t.dtype not in _TYPES:
+        raise PalqError(ERR_ARG, f"no element type for {t.dtype}")
+    return _TYPES[t.dtype], (ld if rows > 1 else max(ld, cols))
+
+
+def _rows3(t, batch, cache, heads_ok=None):
+    """Type, row and head stride of a [tokens, heads, head_dim] tensor of a batch."""
+    tokens, heads, dim = t.shape
+    row, head, one = t.stride()
+    if one != 1 or dim != cache.dim or (heads != cache.heads if heads_ok is None else not heads_ok(heads)):
+        raise PalqError(ERR_ARG, "tensor must be [tokens, heads, head_dim] of the cache, a head's channels consecutive")
+    batch.desc.tokens = tokens
+    if t.dtype not in _TYPES:
+        raise PalqError(ERR_ARG, f"no element type for {t.dtype}")
+    return _TYPES[t.dtype], row, head
 
 
 class ConvPlan:
