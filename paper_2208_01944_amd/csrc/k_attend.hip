@@ -23,6 +23,8 @@
 // them as its second operand.  So probabilities never leave their lane, and V,
 // stored channel by channel, is read 16 tokens at a time.
 #include <algorithm>
+#include <type_traits>
+#include <stdlib.h>
 
 #include "cache.h"
 
@@ -47,6 +49,11 @@ __device__ __forceinline__ h8 codes_h8(uint32_t x, uint32_t y) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// The running maximum moves only when a score passes it by more than 2^8: weights
+// up to 2^8 lose nothing in fp16 or fp32, and most tiles then leave the outputs'
+// accumulators alone.
+constexpr float kSlack = 8.0f;
+
 // One row's reach: tokens [lo, hi).
 struct Reach { int lo, hi; };
 __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Request &q, int t) {
@@ -59,40 +66,50 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Request &q,
   return s;
 }
 
-__device__ __forceinline__ float load_half(const uint16_t *p, bool bf16) { return bf16 ? BF16::get(*p) : F16::get(*p); }
+// The power of two that brings a row's largest magnitude (its bits) to [1, 2),
+// and its inverse.  A row with inf or NaN: 0, so that inf 0 = NaN reaches all of
+// its scores.
+struct RowScale { float in, out; };
+__device__ __forceinline__ RowScale row_scale(uint32_t mag) {
+  const int e = (int)(mag >> 23), b = min(max(e, 1), 253);
+  return {e == 255 ? 0.0f : __uint_as_float((uint32_t)(254 - b) << 23), __uint_as_float((uint32_t)b << 23)};
+}
 
-// A wave's queries: 16 columns, this lane's channels cc D / 4 .. of column
-// lane % 16, scaled to fp16; returns the scale taken out.
-template <class T, int D>
-__device__ __forceinline__ float load_q(const uint16_t *p, bool live, bool vec, h8 *out) {
-  float v[D / 4];
+// 8 n consecutive elements at p (16-byte loads where vec), two in a word.
+template <int N>
+__device__ __forceinline__ void load_words(const uint16_t *p, bool vec, v4i *raw) {
+  if (vec) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) raw[s] = ((const v4i *)p)[s];
+  } else {
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[s][i] = (int)((uint32_t)p[s * 8 + 2 * i] | (uint32_t)p[s * 8 + 2 * i + 1] << 16);
+  }
+}
+template <class T>
+__device__ __forceinline__ float low(int w) { return T::get((uint16_t)((uint32_t)w & 0xffffu)); }
+template <class T>
+__device__ __forceinline__ float high(int w) { return T::get((uint16_t)((uint32_t)w >> 16)); }
+template <class T, int N>
+__device__ __forceinline__ uint32_t largest(const v4i *raw) {
   uint32_t mag = 0;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) {
-    if (live && vec) {
-      const v4i x = ((const v4i *)p)[s];
+  for (int s = 0; s < N; ++s)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[8 * s + 2 * i] = T::get((uint16_t)((uint32_t)x[i] & 0xffffu));
-        v[8 * s + 2 * i + 1] = T::get((uint16_t)((uint32_t)x[i] >> 16));
-      }
-    } else {
+    for (int i = 0; i < 4; ++i) mag = max(mag, max(mag_bits(low<T>(raw[s][i])), mag_bits(high<T>(raw[s][i]))));
+  return mag;
+}
+template <class T>
+__device__ __forceinline__ h8 scaled(v4i raw, float f) {
+  h8 o;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[8 * s + i] = live ? T::get(p[8 * s + i]) : 0.0f;
-    }
+  for (int i = 0; i < 4; ++i) {
+    o[2 * i] = (_Float16)(low<T>(raw[i]) * f);
+    o[2 * i + 1] = (_Float16)(high<T>(raw[i]) * f);
   }
-#pragma unroll
-  for (int i = 0; i < D / 4; ++i) mag = max(mag, mag_bits(v[i]));
-  mag = max(mag, (uint32_t)__shfl_xor((int)mag, 16));
-  mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
-  const int e = max(1, (int)(mag >> 23));  // 2^(e - 127) <= largest; 255: not finite
-  // a row with inf or NaN: inf 0 = NaN, so all its scores are NaN
-  const float f = e == 255 ? 0.0f : __uint_as_float((uint32_t)(254 - min(e, 253)) << 23);
-#pragma unroll
-  for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) out[s][i] = (_Float16)(v[8 * s + i] * f);
-  return __uint_as_float((uint32_t)min(e, 253) << 23);
+  return o;
 }
 
 // NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
@@ -105,6 +122,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4;
   const int h = blockIdx.y, r = blockIdx.z, split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
   const CacheView &cv = a.c;
+  const int heads = cv.heads;
   const Request q = request_of(a.b, r, cv.shift);
   const int rows = q.n * a.group, first = rt * NQ * 16;
   if (first >= rows) return;
@@ -126,8 +144,16 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
     const int row = first + n * 16 + col;
     const bool live = row < rows;
     const int t = live ? row / a.group : 0, g = live ? row - t * a.group : 0;
-    const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * (D / 4);
-    f[n] = load_q<T, D>(p, live, vec, Q[n]) * a.scale;
+    // this lane's channels c D / 4 .. of row lane % 16 (of the first row past the last)
+    v4i raw[KS];
+    load_words<KS>(a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * (D / 4), vec, raw);
+    uint32_t mag = largest<T, KS>(raw);
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 16));
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
+    const RowScale rs = row_scale(mag);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[n][s] = scaled<T>(raw[s], rs.in);
+    f[n] = rs.out * a.scale;
     const Reach s = reach_of(a, q, t);
     rlo[n] = s.lo;
     rhi[n] = live ? s.hi : 0;
@@ -142,66 +168,107 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
     for (int d = 0; d < DT; ++d) O[n][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   }
   const int32_t *table = a.b.table + (int64_t)r * a.b.max_pages;
-  // page of the 16 tokens from `tok` on; -1: no such page
-  auto page_at = [&](int tok) __attribute__((always_inline)) {
-    if (tok >= hi) return -1;
-    const int pid = table[tok >> cv.shift];
-    return pid >= 0 && pid < cv.pages ? pid : -1;
-  };
   const int pm = cv.page - 1;
-  for (int tile = tb + wave; tile < te; tile += 4) {
-    const int t0 = tile << 6;
-    const int kt = t0 + (col >> 2) * 16, vt = t0 + c * 16;  // first token of the chunks this lane loads
-    const int kp = page_at(kt), vp = page_at(vt);
-    const int8_t *kb = cv.k + (((int64_t)max(kp, 0) * cv.heads + h) * cv.page + (kt & pm) + (col & 3)) * D + c * (D / 4);
-    const int8_t *vb = cv.v + (((int64_t)max(vp, 0) * cv.heads + h) * D + col) * cv.page + (vt & pm);
-    const int64_t sc = (int64_t)max(vp, 0) * cv.heads + h;
-    const float ks = cv.ks[sc], vs = cv.vs[sc];
-    uint32_t kx[4][D / 16];
+  // The tile's operands one tile ahead: keys as soon as the scores have taken the
+  // present ones, values after the second product, table entries (checked where
+  // they are used: a branch on them would wait for every load in flight) one
+  // tile before that.
+  const int kc = (col >> 2) * 16, vc = c * 16;  // first tokens of the chunks this lane loads
+  auto entry = [&](int tok) __attribute__((always_inline)) { return table[min(tok, hi - 1) >> cv.shift]; };
+  int kpage = 0, vpage = 0;
+  bool vthere = false;
+  float ks = 0.0f, vs = 0.0f;
+  uint32_t kx[4][D / 16];
+  v4i vx[DT];
+  auto load_k = [&](int tile) __attribute__((always_inline)) {
+    const int kt = tile * 64 + kc, vt = tile * 64 + vc;
+    const bool kok = ((uint32_t)kpage < (uint32_t)cv.pages) & (kt < hi);
+    vthere = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
+    const int8_t *kb = cv.k + (((int64_t)(kok ? kpage : 0) * heads + h) * cv.page + (kt & pm) + (col & 3)) * D + c * (D / 4);
+    const int64_t sc = (int64_t)(vthere ? vpage : 0) * heads + h;
+    ks = cv.ks[sc];
+    vs = cv.vs[sc];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (D % 64 == 0) {
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w) {
+          const v4i x = *(const v4i *)(kb + j * 4 * D + w * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) kx[j][4 * w + i] = (uint32_t)x[i];
+        }
+      } else {
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) {
+          const v2i x = *(const v2i *)(kb + j * 4 * D + w * 8);
+          kx[j][2 * w] = (uint32_t)x[0];
+          kx[j][2 * w + 1] = (uint32_t)x[1];
+        }
+      }
+    }
+  };
+  auto load_v = [&](int tile) __attribute__((always_inline)) {
+    const int vt = tile * 64 + vc;
+    const bool ok = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
+    const int8_t *vb = cv.v + (((int64_t)(ok ? vpage : 0) * heads + h) * D + col) * cv.page + (vt & pm);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) vx[d] = *(const v4i *)(vb + d * 16 * cv.page);
+  };
+  if (tb + wave < te) {
+    kpage = entry((tb + wave) * 64 + kc);
+    vpage = entry((tb + wave) * 64 + vc);
+    load_k(tb + wave);
+    const int nk = entry((tb + wave + 4) * 64 + kc), nv = entry((tb + wave + 4) * 64 + vc);
+    load_v(tb + wave);
+    kpage = nk;
+    vpage = nv;
+  }
+  auto step = [&](int tile, auto last) __attribute__((always_inline)) {
+    constexpr bool more = !decltype(last)::value;
+    const int vt = tile * 64 + vc;
+    const bool there = vthere;
+    const float kst = ks, vst = vs;
+    v4f S[NQ][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int w = 0; w < D / 32; ++w) {
-        const v2i x = *(const v2i *)(kb + (int64_t)j * 4 * D + w * 8);
-        kx[j][2 * w] = (uint32_t)x[0];
-        kx[j][2 * w + 1] = (uint32_t)x[1];
-      }
-    v4i vx[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) vx[d] = *(const v4i *)(vb + (int64_t)d * 16 * cv.page);
-    v4f S[NQ][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-#pragma unroll
       for (int n = 0; n < NQ; ++n) S[n][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
         const h8 A = codes_h8(kx[j][2 * s], kx[j][2 * s + 1]);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) S[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, Q[n][s], S[n][j], 0, 0, 0);
       }
-    }
-    const float u = __builtin_log2f(vs), rv = 1.0f / vs;
+    if constexpr (more) load_k(tile + 4);
+    const float u = __builtin_amdgcn_logf(vst), rv = 1.0f / vst;
     h8 P[NQ][2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-      const float fk = f[n] * ks;
+      const float fk = f[n] * kst;
       float mx = -INFINITY;
+      // (whole tiles need no masks, but rows are few and the test would cost as much)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int tok = vt + 4 * j + i;
-          const bool sees = tok >= rlo[n] && tok < rhi[n] && vp >= 0;
+          const bool sees = there & (tok >= rlo[n]) & (tok < rhi[n]);
           const float s = sees ? __builtin_fmaf(S[n][j][i], fk, u) : -INFINITY;
           S[n][j][i] = s;
           mx = fmaxf(mx, s);
         }
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(M[n], mx), ms = mn == -INFINITY ? 0.0f : mn;
-      const float alpha = exp2_fast(M[n] - ms);
-      M[n] = mn;
+      if (__any(mx > M[n] + kSlack)) {
+        const float mn = fmaxf(M[n], mx), alpha = exp2_fast(M[n] - (mn == -INFINITY ? 0.0f : mn));
+        M[n] = mn;
+        L[n] *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[n][d] *= alpha;
+      }
+      const float ms = M[n] == -INFINITY ? 0.0f : M[n];
       float sum = 0.0f;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -211,20 +278,27 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
           sum += p;
           P[n][j >> 1][(j & 1) * 4 + i] = (_Float16)p;
         }
-      L[n] = L[n] * alpha + (sum == 0.0f ? 0.0f : sum * rv);
-      if (!__all(alpha == 1.0f))
-#pragma unroll
-        for (int d = 0; d < DT; ++d) O[n][d] *= alpha;
+      L[n] += sum == 0.0f ? 0.0f : sum * rv;
     }
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
+      for (int d = 0; d < DT; ++d) {
         const h8 A = codes_h8((uint32_t)vx[d][2 * s], (uint32_t)vx[d][2 * s + 1]);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) O[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, P[n][s], O[n][d], 0, 0, 0);
       }
-  }
+    if constexpr (more) {  // (entries first: loads end in order, and the next keys wait for these)
+      const int nk = entry((tile + 8) * 64 + kc), nv = entry((tile + 8) * 64 + vc);
+      load_v(tile + 4);
+      kpage = nk;
+      vpage = nv;
+    }
+  };
+  // (the last step apart: under a condition, loads would be waited for as if there were none)
+  int tile = tb + wave;
+  for (; tile + 4 < te; tile += 4) step(tile, std::false_type());
+  if (tile < te) step(tile, std::true_type());
 
   // the waves' results under one maximum
 #pragma unroll
@@ -279,6 +353,294 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
   }
 }
 
+// ------------------------------------------------------------ many rows
+// Prompts: a workgroup of W waves takes 32 W (query, head) rows of one cache
+// head, a wave 32 of them on v_mfma_f32_32x32x16_f16, in the layout above (a lane
+// has one query and, of every 32 tokens, 16 consecutive ones).  The workgroup's
+// 64-token tiles are read as codes two tiles ahead, converted to fp16 once and kept
+// in LDS for all waves (two tiles, one barrier each).
+//
+// LDS holds each matrix operand as the 1 KB that a wave reads, lane after lane, so
+// a read is a lane's own address plus a constant and meets no bank twice; the
+// threads that bring a tile are arranged so that 8 neighbours write 8 neighbouring
+// lanes' pieces (row 8 g + 4 c + i of a subtile of keys is token 16 c + 4 g + i).
+//
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int D, int W>
+struct TileLds {
+  static constexpr int KEYS = 64 * D * 2, STAGE = 2 * KEYS;
+  static constexpr int OUT = 32 * W * (D * 2 + 16);  // the epilogue's rows
+  static constexpr int BYTES = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+};
+
+template <class T, int D, int W>
+__global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
+  typedef TileLds<D, W> G;
+  constexpr int TH = 64 * W, KS = D / 16, DT = D / 32, PP = (4 * D + TH - 1) / TH;
+  __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
+  __shared__ float4 blocks[2][4];  // of the tile's 16-token chunks: {ks, log2 vs, 1 / vs, page there}
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, c = lane >> 5;
+  // cache heads go fastest, so a head's tiles share one XCD's L2 where heads are a
+  // multiple of 8; the rows with the longest reach start first
+  const int heads = a.c.heads, combos = heads * a.b.requests;
+  const int combo = blockIdx.x % combos, rest = blockIdx.x / combos;
+  const int h = combo % heads, r = (combo / heads + rest) % a.b.requests, split = rest % a.splits, rt = row_tiles - 1 - rest / a.splits;
+  const CacheView &cv = a.c;
+  const Request q = request_of(a.b, r, cv.shift);
+  const int rows = q.n * a.group, first = rt * 32 * W;
+  if (first >= rows) return;
+  const int last = min(rows, first + 32 * W) - 1;
+  const Reach rf = reach_of(a, q, first / a.group), rl = reach_of(a, q, last / a.group);
+  const int hi = rl.hi;
+  const int tile0 = rf.lo >> 6, ntiles = hi > rf.lo ? ((hi + 63) >> 6) - tile0 : 0;
+  const int per = (ntiles + a.splits - 1) / a.splits;
+  const int tb = tile0 + min(ntiles, split * per), te = tile0 + min(ntiles, (split + 1) * per);
+
+  // this wave's rows
+  const int row = first + wave * 32 + col;
+  const bool live = row < rows;
+  const int t = live ? row / a.group : 0, hq = h * a.group + (live ? row - t * a.group : 0);
+  const Reach mine = reach_of(a, q, t);
+  const int rlo = mine.lo, rhi = live ? mine.hi : 0;
+  // tokens that all of the wave's rows see, and that any sees
+  const int w0 = first + wave * 32, w1 = min(w0 + 31, last);
+  const Reach wf = reach_of(a, q, min(w0, last) / a.group), wl = reach_of(a, q, w1 / a.group);
+  const int all_lo = wl.lo, all_hi = w0 + 31 <= last ? wf.hi : 0, any_lo = wf.lo, any_hi = w0 <= last ? wl.hi : 0;
+
+  h8 Q[KS];
+  float f;
+  {
+    const bool vec = (((uintptr_t)a.q | (uintptr_t)(a.q_row * 2) | (uintptr_t)(a.q_head * 2)) & 15u) == 0;
+    const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)hq * a.q_head + c * 8;
+    v4i raw[KS];
+    if (vec) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) raw[s] = *(const v4i *)(p + s * 16);
+    } else {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) load_words<1>(p + s * 16, false, &raw[s]);
+    }
+    uint32_t mag = largest<T, KS>(raw);
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
+    RowScale rs = row_scale(mag);
+    if (a.scale < 0.0f) rs.in = -rs.in;  // the factor of the products stays >= 0
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[s] = scaled<T>(raw[s], rs.in);
+    f = rs.out * fabsf(a.scale);
+  }
+
+  const int32_t *table = a.b.table + (int64_t)r * a.b.max_pages;
+  const int pm = cv.page - 1;
+  // table entry of a token's page (of the last token's past it), checked only where
+  // it is used: a branch on it here would wait for every load in flight
+  auto entry = [&](int tok) __attribute__((always_inline)) { return table[min(tok, hi - 1) >> cv.shift]; };
+  auto there = [&](int pid, int tok) __attribute__((always_inline)) { return ((uint32_t)pid < (uint32_t)cv.pages) & (tok < hi); };
+  // the 16-byte pieces that this thread brings of a tile: 16 channels of a key, 16 tokens of a value channel
+  struct Entries { int k[PP], v[PP], b; } pages[2];
+  v4i kx[2][PP], vx[2][PP];
+  float3 bx[2];  // ks, vs, page there
+  struct Piece { int tok, s, kr, d, vt; };  // key's token, 16 channels, matrix row; value's channel, first token
+  auto piece = [&](int i) __attribute__((always_inline)) {
+    const int p = threadIdx.x + i * TH, j = p & 7, s = p / 8 % KS, gu = p / (8 * KS), g = gu & 3, u = gu >> 2;
+    return Piece{u * 32 + (j >> 2) * 16 + g * 4 + (j & 3), s, u * 32 + g * 8 + j, (p >> 6) * 16 + (p & 15), (p >> 4 & 3) * 16};
+  };
+  auto none = [&](int i) __attribute__((always_inline)) { return 4 * D % TH && (int)threadIdx.x + i * TH >= 4 * D; };
+  auto entries = [&](int tile, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PP; ++i) {
+      const Piece p = piece(i);
+      pages[buf].k[i] = entry(tile * 64 + p.tok);
+      pages[buf].v[i] = entry(tile * 64 + p.vt);
+    }
+    pages[buf].b = entry(tile * 64 + (threadIdx.x & 3) * 16);
+  };
+  auto load = [&](int tile, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PP; ++i) {
+      const Piece p = piece(i);
+      const int64_t kh = (int64_t)(there(pages[buf].k[i], tile * 64 + p.tok) ? pages[buf].k[i] : 0) * heads + h;
+      const int64_t vh = (int64_t)(there(pages[buf].v[i], tile * 64 + p.vt) ? pages[buf].v[i] : 0) * heads + h;
+      const int in = (tile * 64) & pm;
+      kx[buf][i] = *(const v4i *)(cv.k + (kh << cv.shift) * D + ((in + p.tok) & pm) * D + p.s * 16);
+      vx[buf][i] = *(const v4i *)(cv.v + (vh << cv.shift) * D + (p.d << cv.shift) + ((in + p.vt) & pm));
+    }
+    const bool page = there(pages[buf].b, tile * 64 + (threadIdx.x & 3) * 16);
+    const int64_t at = (int64_t)(page ? pages[buf].b : 0) * heads + h;
+    bx[buf] = make_float3(cv.ks[at], cv.vs[at], page ? 1.0f : 0.0f);
+  };
+  auto put = [&](int buf) __attribute__((always_inline)) {
+    uint8_t *base = lds + buf * G::STAGE;
+#pragma unroll
+    for (int i = 0; i < PP; ++i) {
+      if (none(i)) break;
+      const Piece p = piece(i);
+      // operand (subtile, 16 channels): lane 32 c + row has 8 channels from 8 c
+      uint8_t *kd = base + ((p.kr >> 5) * KS + p.s) * 1024 + (p.kr & 31) * 16;
+      *(h8 *)kd = codes_h8((uint32_t)kx[buf][i][0], (uint32_t)kx[buf][i][1]);
+      *(h8 *)(kd + 512) = codes_h8((uint32_t)kx[buf][i][2], (uint32_t)kx[buf][i][3]);
+      // operand (32 channels, subtile, k): lane 32 c + channel has 8 tokens from 16 c + 8 k
+      uint8_t *vd = base + G::KEYS + (p.d >> 5) * 4096 + (p.vt >> 5) * 2048 + (p.vt >> 4 & 1) * 512 + (p.d & 31) * 16;
+      *(h8 *)vd = codes_h8((uint32_t)vx[buf][i][0], (uint32_t)vx[buf][i][1]);
+      *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[buf][i][2], (uint32_t)vx[buf][i][3]);
+    }
+    if (threadIdx.x < 4) blocks[buf][threadIdx.x] = make_float4(bx[buf].x, __builtin_amdgcn_logf(bx[buf].y), 1.0f / bx[buf].y, bx[buf].z);
+  };
+
+  v16f O[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) O[d][i] = 0.0f;
+  float M = -INFINITY, L = 0.0f;
+
+  if (tb < te) {
+    entries(tb, 0);
+    entries(tb + 1, 1);
+    load(tb, 0);
+    entries(tb + 2, 0);
+    load(tb + 1, 1);
+    put(0);
+  }
+  __syncthreads();
+  const uint8_t *mylds = lds + lane * 16;
+  auto step = [&](int tile, auto which) __attribute__((always_inline)) {
+    constexpr int buf = decltype(which)::value;
+    const int t0 = tile * 64;
+    // Loads end in order: the entries that the next step needs come before this
+    // step's data.  None of it stands under a condition, so that waits count only
+    // what they need; past the last tile it reads tiles that nobody uses.
+    entries(tile + 3, buf ^ 1);
+    load(tile + 2, buf);
+    if (t0 < any_hi && t0 + 64 > any_lo) {
+      v16f S[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[u][i] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          S[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + buf * G::STAGE + (u * KS + s) * 1024), Q[s], S[u], 0, 0, 0);
+      const float4 b0 = blocks[buf][c], b1 = blocks[buf][2 + c];
+      // tokens of this lane that its row does not see, where there are any
+      const bool masked = !(__all(b0.w != 0.0f && b1.w != 0.0f) && t0 >= all_lo && t0 + 64 <= all_hi);
+      uint32_t off = 0;
+      if (masked) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const bool ok = (u ? b1.w : b0.w) != 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int tok = t0 + u * 32 + c * 16 + i;
+            const bool sees = ok & (tok >= rlo) & (tok < rhi);
+            off |= sees ? 0u : 1u << (u * 16 + i);
+            S[u][i] = sees ? S[u][i] : -INFINITY;
+          }
+        }
+      }
+      // s fk + lv, fk >= 0: the largest comes from the largest product
+      const float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m = fmaxf(m, S[u][i]);
+        mx = fmaxf(mx, m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[u], lv[u]));
+      }
+      mx = other_half_max(mx);
+      if (__any(mx > M + kSlack)) {
+        const float mn = fmaxf(M, mx), alpha = exp2_fast(M - (mn == -INFINITY ? 0.0f : mn));
+        M = mn;
+        L *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[d] *= alpha;
+      }
+      const float ms = M == -INFINITY ? 0.0f : M;
+      h8 P[2][2];
+      auto weights = [&](auto some) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float o = lv[u] - ms;
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float p = exp2_fast(__builtin_fmaf(S[u][i], fk[u], o));
+            if constexpr (decltype(some)::value) p = off >> (u * 16 + i) & 1u ? 0.0f : p;
+            sum += p;
+            P[u][i >> 3][i & 7] = (_Float16)p;
+          }
+          L += sum == 0.0f ? 0.0f : sum * (u ? b1.z : b0.z);
+        }
+      };
+      if (masked) weights(std::true_type());
+      else weights(std::false_type());
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + buf * G::STAGE + G::KEYS + d * 4096 + k * 1024),
+                                                         P[k >> 1][k & 1], O[d], 0, 0, 0);
+    }
+    put(buf ^ 1);
+    __syncthreads();
+  };
+  for (int tile = tb; tile < te; tile += 2) {
+    step(tile, std::integral_constant<int, 0>());
+    if (tile + 1 < te) step(tile + 1, std::integral_constant<int, 1>());
+  }
+
+  L += __shfl_xor(L, 32);
+  if (a.splits > 1) {
+    if (!live) return;
+    const int64_t hs = (int64_t)heads * a.group, at = ((int64_t)split * a.b.tokens + q.row0 + t) * hs + hq;
+    float *dst = a.part + at * D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(v4f *)(dst + d * 32 + g * 8 + c * 4) = v4f{O[d][4 * g], O[d][4 * g + 1], O[d][4 * g + 2], O[d][4 * g + 3]};
+    if (c == 0) {
+      float *ml = a.part + (int64_t)a.splits * a.b.tokens * hs * D + at * 2;
+      ml[0] = M;
+      ml[1] = L;
+    }
+    return;
+  }
+  // rows through LDS (the last barrier came after every wave's last read), a wave's own part
+  const float inv = L == 0.0f ? 0.0f : 1.0f / L;
+  constexpr int LD = D + 8;
+  uint16_t *my = (uint16_t *)lds + wave * 32 * LD;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float v[4] = {O[d][4 * g] * inv, O[d][4 * g + 1] * inv, O[d][4 * g + 2] * inv, O[d][4 * g + 3] * inv};
+      store4<T>(my + col * LD + d * 32 + g * 8 + c * 4, v, true);
+    }
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const bool vec = (((uintptr_t)a.out | (uintptr_t)(a.out_row * 2) | (uintptr_t)(a.out_head * 2)) & 15u) == 0;
+  for (int p = lane; p < 32 * (D / 8); p += 64) {
+    const int rr = p / (D / 8), e = p % (D / 8) * 8, orow = first + wave * 32 + rr;
+    if (orow >= rows) continue;
+    const int ot = orow / a.group, oh = h * a.group + orow - ot * a.group;
+    const v4i o = *(const v4i *)(my + rr * LD + e);
+    uint16_t *dst = a.out + (q.row0 + ot) * a.out_row + (int64_t)oh * a.out_head + e;
+    if (vec) {
+      *(v4i *)dst = o;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dst[i] = (uint16_t)((uint32_t)o[i >> 1] >> (16 * (i & 1)));
+    }
+  }
+}
+
 // One (token, head) row a group of D / 4 threads: the splits under one maximum.
 template <class T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
@@ -305,20 +667,29 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store4<T>(dst, v, (((uintptr_t)a.out | (uintptr_t)(a.out_row * 2) | (uintptr_t)(a.out_head * 2)) & 7u) == 0);
 }
 
-// Row tiles of a workgroup in the kernel's NQ.
-int row_tiles(const AttendArgs &a) {
+// Rows of a workgroup: 16, 32 or 64 on attend_rows_kernel, 32 a wave on attend_tile_kernel.
+int block_rows(const AttendArgs &a) {
   const int64_t rows = (int64_t)a.b.max_new * a.group;
-  return rows <= 16 ? 1 : rows <= 32 || a.c.dim == 256 ? 2 : 4;
+  static const char *force = getenv("PQ_ROWS");
+  if (force) return atoi(force);
+  if (rows <= 32) return rows <= 16 ? 16 : 32;
+  return rows <= 128 || a.c.dim == 256 ? 128 : 256;
 }
 
 template <class T, int D>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
-  const int nq = row_tiles(a);
-  const int64_t rows = (int64_t)a.b.max_new * a.group;
-  const dim3 g((unsigned)((rows + nq * 16 - 1) / (nq * 16) * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
-  if (nq == 1) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
-  else if (nq == 2) attend_rows_kernel<T, D, 2><<<g, 256, 0, s>>>(a);
-  else if constexpr (D < 256) attend_rows_kernel<T, D, 4><<<g, 256, 0, s>>>(a);
+  const int br = block_rows(a);
+  const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + br - 1) / br;
+  if (br >= 128) {
+    const unsigned g = (unsigned)(rt * a.splits * a.c.heads * a.b.requests);
+    if (br == 128) attend_tile_kernel<T, D, 4><<<g, 256, 0, s>>>(a, (int)rt);
+    else if constexpr (D < 256) attend_tile_kernel<T, D, 8><<<g, 512, 0, s>>>(a, (int)rt);
+  } else {
+    const dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
+    if (br == 16) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
+    else if (br == 32) attend_rows_kernel<T, D, 2><<<g, 256, 0, s>>>(a);
+    else if constexpr (D < 256) attend_rows_kernel<T, D, 4><<<g, 256, 0, s>>>(a);
+  }
   if (a.splits > 1) {
     const int64_t per = 256 / (D / 4), n = (int64_t)a.b.max_new * a.c.heads * a.group;
     attend_join_kernel<T, D><<<dim3((unsigned)((n + per - 1) / per), (unsigned)a.b.requests), 256, 0, s>>>(a);
@@ -339,7 +710,7 @@ hipError_t launch_attend_t(const AttendArgs &a, hipStream_t s) {
 }  // namespace
 
 void attend_plan(AttendArgs &a, int cus) {
-  const int64_t rows = (int64_t)a.b.max_new * a.group, nq = row_tiles(a) * 16;
+  const int64_t rows = (int64_t)a.b.max_new * a.group, nq = block_rows(a);
   const int64_t base = std::max<int64_t>(1, (rows + nq - 1) / nq * a.c.heads * a.b.requests);
   // every wave at least one tile of 64 tokens
   const int64_t most = std::max<int64_t>(1, (a.b.max_len + 255) / 256);

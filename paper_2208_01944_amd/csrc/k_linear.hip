@@ -10,6 +10,7 @@
 // follow each other along k, then along rows.  k is padded to whole blocks
 // with zero codes, rows to whole tiles with rows whose results are not stored.
 #include <algorithm>
+#include <stdlib.h>
 
 #include "linear.h"
 #include "serve_common.h"
@@ -164,10 +165,198 @@ __global__ __launch_bounds__(256) void linear_few_kernel(LinearArgs a) {
   }
 }
 
+// ------------------------------------------------------------ many tokens
+// A workgroup of WC x WT waves takes 32 CT WC channels x 32 TT WT tokens, a
+// wave 32 CT x 32 TT of them on v_mfma_i32_32x32x32_i8.  k goes by stages of 128:
+// both operands' slabs are copied from memory straight into LDS (two stages, one
+// in use, one on its way), and a wave reads the operands of the next 32 k while
+// the matrix cores work on the present ones, across the stage's barrier too.
+constexpr int kStageK = 128;
+
+// 16 bytes per lane from the buffer into LDS at `dst` (uniform) + 16 lane; in asm,
+// so that the compiler does not order LDS reads after them: the stages' waits and
+// barriers do.
+__device__ __forceinline__ void to_lds(v4i rsrc, uint32_t dst, uint32_t voff, uint32_t soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "s"(dst), "v"(voff), "s"(rsrc), "s"(soff)
+               : "m0");
+}
+__device__ __forceinline__ v4i buffer_of(const void *base) {
+  const uint64_t p = (uint64_t)base;
+  return v4i{__builtin_amdgcn_readfirstlane((int)(uint32_t)p), __builtin_amdgcn_readfirstlane((int)((uint32_t)(p >> 32) & 0xffffu)),
+             -1, 0x00020000};
+}
+// All of this wave's loads and LDS reads done, then the workgroup's.
+__device__ __forceinline__ void stage_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int WC, int WT, int CT, int TT>
+struct TileShape {
+  static constexpr int C = 32 * CT * WC, M = 32 * TT * WT, WAVES = WC * WT;
+  static constexpr int STAGE = (C + M) * kStageK;                   // bytes of one stage
+  static constexpr int OUT = 32 * (32 * CT + 4) * 4 * WAVES;        // the epilogue's: 32 tokens of every wave
+  static constexpr int LDS = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+};
+
+template <class T, int WC, int WT, int CT, int TT, int WPE>
+__global__ __launch_bounds__(64 * WC * WT, WPE) void linear_tile_kernel(LinearArgs a, int ctiles, int mtiles, int band) {
+  typedef TileShape<WC, WT, CT, TT> G;
+  typedef typename T::raw R;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[G::LDS];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wc = wave % WC, wt = wave / WC;
+
+  // Workgroup i runs on XCD i % 8: each XCD takes a contiguous run of the tiles,
+  // which go by bands of `band` token tiles, so that the tiles of an XCD at a
+  // time share rows of both operands in its L2.
+  const int tiles = ctiles * mtiles, per = (tiles + 7) / 8;
+  const int t = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if (t >= tiles || (int)(blockIdx.x >> 3) >= per) return;
+  const int b0 = t / (band * ctiles) * band, inb = min(band, mtiles - b0), rem = t - b0 * ctiles;
+  const int ct0 = rem / inb, mt0 = b0 + rem % inb;
+
+  const int kb = a.kp / 64, stages = a.kp / kStageK;
+  const v4i rw = buffer_of(a.w + (int64_t)ct0 * (G::C / 16) * kb * 1024);
+  const v4i rx = buffer_of(a.x + (int64_t)mt0 * (G::M / 16) * kb * 1024);
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
+  // a stage in LDS: 16-row slabs of the channels, then of the tokens, two slabs (128 k) each
+  constexpr int LOADS = (G::C + G::M) / 16 * 2;
+  auto fetch = [&](int s) __attribute__((always_inline)) {
+    const uint32_t at = base + (uint32_t)(s & 1) * G::STAGE;
+#pragma unroll
+    for (int i = 0; i < (LOADS + G::WAVES - 1) / G::WAVES; ++i) {
+      const int piece = i * G::WAVES + wave;  // uniform
+      if (LOADS % G::WAVES && piece >= LOADS) break;
+      const int slab = piece >> 1;
+      const bool w = slab < G::C / 16;
+      const uint32_t soff = (uint32_t)(((w ? slab : slab - G::C / 16) * kb + 2 * s + (piece & 1)) * 1024);
+      to_lds(w ? rw : rx, at + piece * 1024, lane * 16, soff);
+    }
+  };
+  // operands of 32 k: lane l has row l % 32, 16 k from l / 32
+  struct Ops { v4i w[CT], x[TT]; };
+  const int lo = (lane & 15) * 16 + (lane >> 4 & 1) * 2048 + (lane >> 5) * 256;
+  const int wo = lo + wc * CT * 4096, xo = lo + G::C * kStageK + wt * TT * 4096;
+  auto read = [&](Ops &o, int s, int step) __attribute__((always_inline)) {
+    const uint8_t *p = lds + (s & 1) * G::STAGE + (step >> 1) * 1024 + (step & 1) * 512;
+#pragma unroll
+    for (int c = 0; c < CT; ++c) o.w[c] = *(const v4i *)(p + wo + c * 4096);
+#pragma unroll
+    for (int m = 0; m < TT; ++m) o.x[m] = *(const v4i *)(p + xo + m * 4096);
+  };
+  v16i acc[CT][TT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c)
+#pragma unroll
+    for (int m = 0; m < TT; ++m)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[c][m][i] = 0;
+  auto multiply = [&](const Ops &o) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < TT; ++m)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) acc[c][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.w[c], o.x[m], acc[c][m], 0, 0, 0);
+  };
+
+  Ops ops[2];
+  fetch(0);
+  stage_barrier();
+  if (stages > 1) fetch(1);
+  read(ops[0], 0, 0);
+  for (int s = 0; s < stages; ++s) {
+    read(ops[1], s, 1);
+    multiply(ops[0]);
+    read(ops[0], s, 2);
+    multiply(ops[1]);
+    read(ops[1], s, 3);
+    multiply(ops[0]);
+    // every read of stage s is done: its place takes stage s + 2
+    stage_barrier();
+    if (s + 1 < stages) {
+      if (s + 2 < stages) fetch(s + 2);
+      read(ops[0], s + 1, 0);
+    }
+    multiply(ops[1]);
+  }
+
+  // 32 tokens at a time through a part of LDS that is the wave's own (the last
+  // barrier came after every wave's last read), so that rows leave whole.  The
+  // lane has token lane % 32 and channels 8 g + 4 (lane / 32) + i of each tile.
+  constexpr int CW = 32 * CT, LD = CW + 16 / (int)sizeof(R);  // channels of the wave; a row's elements in LDS
+  constexpr int E = 16 / (int)sizeof(R);                      // elements of a 16-byte store
+  R *mine = (R *)(lds + wave * (G::OUT / G::WAVES));
+  const int c0 = ct0 * G::C + wc * CW;
+  const bool vec = (((uintptr_t)a.y | (uintptr_t)(a.y_ld * (int64_t)sizeof(R))) & 15u) == 0;
+#pragma unroll
+  for (int m = 0; m < TT; ++m) {
+    const int64_t row0 = (int64_t)mt0 * G::M + (wt * TT + m) * 32;
+    if (row0 >= a.rows) break;
+    const float xs = a.x_scale[min(row0 + (lane & 31), a.rows - 1)];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int ch = c * 32 + g * 8 + (lane >> 5) * 4;
+        const v4f ws = *(const v4f *)(a.w_scale + c0 + ch);
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (float)acc[c][m][g * 4 + i] * xs * ws[i];
+        if (a.bias) {
+          const v4f b = *(const v4f *)(a.bias + c0 + ch);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] += b[i];
+        }
+        store4<T>(mine + (lane & 31) * LD + ch, v, true);
+      }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int PR = CW / E;  // 16-byte pieces of a row
+#pragma unroll
+    for (int p = 0; p < 32 * PR / 64; ++p) {
+      const int piece = p * 64 + lane, r = piece / PR, e = piece % PR * E;
+      const v4i o = *(const v4i *)(mine + r * LD + e);
+      const int64_t row = row0 + r;
+      const int n = c0 + e;
+      if (row >= a.rows || n >= a.n_out) continue;
+      R *y = (R *)a.y + row * a.y_ld + n;
+      if (vec && n + E <= a.n_out) {
+        *(v4i *)y = o;
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (n + i < a.n_out) {
+            if constexpr (sizeof(R) == 4) y[i] = __int_as_float(o[i]);
+            else y[i] = (R)((uint32_t)o[i >> 1] >> (16 * (i & 1)));
+          }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+template <class T, int WC, int WT, int CT, int TT, int WPE>
+hipError_t launch_tile(const LinearArgs &a, hipStream_t s) {
+  typedef TileShape<WC, WT, CT, TT> G;
+  const int ctiles = (a.n_out + G::C - 1) / G::C, mtiles = (int)((a.rows + G::M - 1) / G::M);
+  const int per = (ctiles * mtiles + 7) / 8;
+  linear_tile_kernel<T, WC, WT, CT, TT, WPE><<<(unsigned)(per * 8), 64 * WC * WT, 0, s>>>(a, ctiles, mtiles, 4);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t launch_linear_t(const LinearArgs &a, hipStream_t s) {
   const unsigned nt = (unsigned)((a.n_out + 15) / 16);
   const int64_t mt = (a.rows + 15) / 16;
+  static const char *force = getenv("PQ_TILE");
+  const int f = force ? atoi(force) : 0;
+  if (f == 1) return launch_tile<T, 2, 2, 4, 4, 1>(a, s);
+  if (f == 2) return launch_tile<T, 2, 4, 4, 2, 2>(a, s);
+  if (f == 3) return launch_tile<T, 2, 2, 2, 2, 2>(a, s);
+  if (f == 4) return launch_tile<T, 2, 2, 1, 1, 2>(a, s);
+  if (f == 5) return launch_tile<T, 2, 2, 4, 2, 1>(a, s);
+  if (f == 6) return launch_tile<T, 2, 2, 2, 1, 2>(a, s);
+  if (f == 7) return launch_tile<T, 4, 2, 2, 4, 2>(a, s);
   if (mt <= 1) linear_few_kernel<T, 1><<<dim3(nt, 1), 256, 0, s>>>(a);
   else if (mt <= 2) linear_few_kernel<T, 2><<<dim3(nt, 1), 256, 0, s>>>(a);
   else linear_few_kernel<T, 4><<<dim3(nt, (unsigned)((mt + 3) / 4)), 256, 0, s>>>(a);
