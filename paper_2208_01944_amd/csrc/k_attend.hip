@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
   // they are used: a branch on them would wait for every load in flight) one
   // tile before that.
   const int kc = (col >> 2) * 16, vc = c * 16;  // first tokens of the chunks this lane loads
-  auto entry = [&](int tok) __attribute__((always_inline)) { return table[min(tok, hi - 1) >> cv.shift]; };
+  auto entry = [&](int tok) __attribute__((always_inline)) { return table[(uint32_t)min(tok, hi - 1) >> cv.shift]; };
   int kpage = 0, vpage = 0;
   bool vthere = false;
   float ks = 0.0f, vs = 0.0f;
@@ -207,10 +207,15 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
       }
     }
   };
+  // the next values, and the table entries of the tile after: loads end in order and
+  // the next keys wait for the entries, so these come first (into the registers that
+  // the values' address has just left)
   auto load_v = [&](int tile) __attribute__((always_inline)) {
     const int vt = tile * 64 + vc;
     const bool ok = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
     const int8_t *vb = cv.v + (((int64_t)(ok ? vpage : 0) * heads + h) * D + col) * cv.page + (vt & pm);
+    kpage = entry((tile + 4) * 64 + kc);
+    vpage = entry((tile + 4) * 64 + vc);
 #pragma unroll
     for (int d = 0; d < DT; ++d) vx[d] = *(const v4i *)(vb + d * 16 * cv.page);
   };
@@ -218,10 +223,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
     kpage = entry((tb + wave) * 64 + kc);
     vpage = entry((tb + wave) * 64 + vc);
     load_k(tb + wave);
-    const int nk = entry((tb + wave + 4) * 64 + kc), nv = entry((tb + wave + 4) * 64 + vc);
     load_v(tb + wave);
-    kpage = nk;
-    vpage = nv;
   }
   auto step = [&](int tile, auto last) __attribute__((always_inline)) {
     constexpr bool more = !decltype(last)::value;
@@ -288,12 +290,7 @@ __global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
 #pragma unroll
         for (int n = 0; n < NQ; ++n) O[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, P[n][s], O[n][d], 0, 0, 0);
       }
-    if constexpr (more) {  // (entries first: loads end in order, and the next keys wait for these)
-      const int nk = entry((tile + 8) * 64 + kc), nv = entry((tile + 8) * 64 + vc);
-      load_v(tile + 4);
-      kpage = nk;
-      vpage = nv;
-    }
+    if constexpr (more) load_v(tile + 4);
   };
   // (the last step apart: under a condition, loads would be waited for as if there were none)
   int tile = tb + wave;
@@ -372,9 +369,9 @@ __device__ __forceinline__ float other_half_max(float x) {
 
 template <int D, int W>
 struct TileLds {
-  static constexpr int KEYS = 64 * D * 2, STAGE = 2 * KEYS;
+  static constexpr int KEYS = 64 * D * 2;            // bytes of a tile's keys, and of its values
   static constexpr int OUT = 32 * W * (D * 2 + 16);  // the epilogue's rows
-  static constexpr int BYTES = 2 * STAGE > OUT ? 2 * STAGE : OUT;
+  static constexpr int BYTES = 4 * KEYS > OUT ? 4 * KEYS : OUT;
 };
 
 template <class T, int D, int W>
@@ -437,57 +434,70 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   const int pm = cv.page - 1;
   // table entry of a token's page (of the last token's past it), checked only where
   // it is used: a branch on it here would wait for every load in flight
-  auto entry = [&](int tok) __attribute__((always_inline)) { return table[min(tok, hi - 1) >> cv.shift]; };
-  auto there = [&](int pid, int tok) __attribute__((always_inline)) { return ((uint32_t)pid < (uint32_t)cv.pages) & (tok < hi); };
-  // the 16-byte pieces that this thread brings of a tile: 16 channels of a key, 16 tokens of a value channel
-  struct Entries { int k[PP], v[PP], b; } pages[2];
-  v4i kx[2][PP], vx[2][PP];
-  float3 bx[2];  // ks, vs, page there
+  auto entry = [&](int tok) __attribute__((always_inline)) { return table[(uint32_t)min(tok, hi - 1) >> cv.shift]; };
+  auto valid = [&](int pid) __attribute__((always_inline)) { return (uint32_t)pid < (uint32_t)cv.pages; };
+  // The 16-byte pieces that this thread brings: 16 channels of a key of tile p and 16
+  // tokens of a value channel of tile p - 1.
   struct Piece { int tok, s, kr, d, vt; };  // key's token, 16 channels, matrix row; value's channel, first token
   auto piece = [&](int i) __attribute__((always_inline)) {
     const int p = threadIdx.x + i * TH, j = p & 7, s = p / 8 % KS, gu = p / (8 * KS), g = gu & 3, u = gu >> 2;
     return Piece{u * 32 + (j >> 2) * 16 + g * 4 + (j & 3), s, u * 32 + g * 8 + j, (p >> 6) * 16 + (p & 15), (p >> 4 & 3) * 16};
   };
   auto none = [&](int i) __attribute__((always_inline)) { return 4 * D % TH && (int)threadIdx.x + i * TH >= 4 * D; };
-  auto entries = [&](int tile, int buf) __attribute__((always_inline)) {
+  // Table entries go through two sets of registers by the tile's parity (a copy from
+  // one to the other would wait for them, and so for every load before them).
+  struct Entries { int k[PP], v[PP], b; } ent[2];
+  v4i kx[PP], vx[PP];
+  float bks, bvs, bthere;  // of chunk threadIdx.x % 4 of tile p
+  const uint32_t page_bytes = (uint32_t)heads << cv.shift;  // (times D)
+  const int8_t *kh = cv.k + ((int64_t)h << cv.shift) * D, *vh = cv.v + ((int64_t)h << cv.shift) * D;
+  auto entries = [&](int p, Entries &e) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
-      const Piece p = piece(i);
-      pages[buf].k[i] = entry(tile * 64 + p.tok);
-      pages[buf].v[i] = entry(tile * 64 + p.vt);
+      e.k[i] = entry(p * 64 + piece(i).tok);
+      e.v[i] = entry(max(p - 1, tb) * 64 + piece(i).vt);
     }
-    pages[buf].b = entry(tile * 64 + (threadIdx.x & 3) * 16);
+    e.b = entry(p * 64 + (threadIdx.x & 3) * 16);
   };
-  auto load = [&](int tile, int buf) __attribute__((always_inline)) {
+  auto load = [&](int p, const Entries &e) __attribute__((always_inline)) {
+    const int ktile = p * 64 & pm, vtile = max(p - 1, tb) * 64 & pm;  // of a page that is wider than a tile
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
-      const Piece p = piece(i);
-      const int64_t kh = (int64_t)(there(pages[buf].k[i], tile * 64 + p.tok) ? pages[buf].k[i] : 0) * heads + h;
-      const int64_t vh = (int64_t)(there(pages[buf].v[i], tile * 64 + p.vt) ? pages[buf].v[i] : 0) * heads + h;
-      const int in = (tile * 64) & pm;
-      kx[buf][i] = *(const v4i *)(cv.k + (kh << cv.shift) * D + ((in + p.tok) & pm) * D + p.s * 16);
-      vx[buf][i] = *(const v4i *)(cv.v + (vh << cv.shift) * D + (p.d << cv.shift) + ((in + p.vt) & pm));
+      const Piece pc = piece(i);
+      const uint64_t kp = (uint64_t)(uint32_t)(valid(e.k[i]) ? e.k[i] : 0) * page_bytes * D;
+      const uint64_t vp = (uint64_t)(uint32_t)(valid(e.v[i]) ? e.v[i] : 0) * page_bytes * D;
+      kx[i] = *(const v4i *)(kh + kp + (uint32_t)((ktile + (pc.tok & pm)) * D + pc.s * 16));
+      vx[i] = *(const v4i *)(vh + vp + (uint32_t)((pc.d << cv.shift) + vtile + (pc.vt & pm)));
     }
-    const bool page = there(pages[buf].b, tile * 64 + (threadIdx.x & 3) * 16);
-    const int64_t at = (int64_t)(page ? pages[buf].b : 0) * heads + h;
-    bx[buf] = make_float3(cv.ks[at], cv.vs[at], page ? 1.0f : 0.0f);
+    const bool page = valid(e.b);
+    const int64_t at = (int64_t)(page ? e.b : 0) * heads + h;
+    bks = cv.ks[at];
+    bvs = cv.vs[at];
+    bthere = page ? 1.0f : 0.0f;
   };
-  auto put = [&](int buf) __attribute__((always_inline)) {
-    uint8_t *base = lds + buf * G::STAGE;
+  // keys of tile p and values of tile p - 1 to their places, then the loads of the
+  // next.  Loads end in order, so the entries that the next call needs come first.
+  // None of it stands under a condition, so that waits count only what they need; past
+  // the last tile it reads tiles that nobody uses.  par: p - tb is odd.
+  auto bring = [&](int p, auto par) __attribute__((always_inline)) {
+    constexpr int odd = decltype(par)::value;
+    uint8_t *kbase = lds + odd * G::KEYS, *vbase = lds + (2 + (odd ^ 1)) * G::KEYS;
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
       if (none(i)) break;
-      const Piece p = piece(i);
+      const Piece pc = piece(i);
       // operand (subtile, 16 channels): lane 32 c + row has 8 channels from 8 c
-      uint8_t *kd = base + ((p.kr >> 5) * KS + p.s) * 1024 + (p.kr & 31) * 16;
-      *(h8 *)kd = codes_h8((uint32_t)kx[buf][i][0], (uint32_t)kx[buf][i][1]);
-      *(h8 *)(kd + 512) = codes_h8((uint32_t)kx[buf][i][2], (uint32_t)kx[buf][i][3]);
+      uint8_t *kd = kbase + ((pc.kr >> 5) * KS + pc.s) * 1024 + (pc.kr & 31) * 16;
+      *(h8 *)kd = codes_h8((uint32_t)kx[i][0], (uint32_t)kx[i][1]);
+      *(h8 *)(kd + 512) = codes_h8((uint32_t)kx[i][2], (uint32_t)kx[i][3]);
       // operand (32 channels, subtile, k): lane 32 c + channel has 8 tokens from 16 c + 8 k
-      uint8_t *vd = base + G::KEYS + (p.d >> 5) * 4096 + (p.vt >> 5) * 2048 + (p.vt >> 4 & 1) * 512 + (p.d & 31) * 16;
-      *(h8 *)vd = codes_h8((uint32_t)vx[buf][i][0], (uint32_t)vx[buf][i][1]);
-      *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[buf][i][2], (uint32_t)vx[buf][i][3]);
+      uint8_t *vd = vbase + (pc.d >> 5) * 4096 + (pc.vt >> 5) * 2048 + (pc.vt >> 4 & 1) * 512 + (pc.d & 31) * 16;
+      *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1]);
+      *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3]);
     }
-    if (threadIdx.x < 4) blocks[buf][threadIdx.x] = make_float4(bx[buf].x, __builtin_amdgcn_logf(bx[buf].y), 1.0f / bx[buf].y, bx[buf].z);
+    if (threadIdx.x < 4) blocks[odd][threadIdx.x] = make_float4(bks, __builtin_amdgcn_logf(bvs), 1.0f / bvs, bthere);
+    entries(p + 2, ent[odd]);
+    load(p + 1, ent[odd ^ 1]);
   };
 
   v16f O[DT];
@@ -496,104 +506,135 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
 #pragma unroll
     for (int i = 0; i < 16; ++i) O[d][i] = 0.0f;
   float M = -INFINITY, L = 0.0f;
-
-  if (tb < te) {
-    entries(tb, 0);
-    entries(tb + 1, 1);
-    load(tb, 0);
-    entries(tb + 2, 0);
-    load(tb + 1, 1);
-    put(0);
-  }
-  __syncthreads();
+  v16f S[2];
+  h8 P[2][2];
+  bool busy = false;  // this wave has scores, or weights, of the present tile
   const uint8_t *mylds = lds + lane * 16;
-  auto step = [&](int tile, auto which) __attribute__((always_inline)) {
-    constexpr int buf = decltype(which)::value;
-    const int t0 = tile * 64;
-    // Loads end in order: the entries that the next step needs come before this
-    // step's data.  None of it stands under a condition, so that waits count only
-    // what they need; past the last tile it reads tiles that nobody uses.
-    entries(tile + 3, buf ^ 1);
-    load(tile + 2, buf);
-    if (t0 < any_hi && t0 + 64 > any_lo) {
-      v16f S[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S[u][i] = 0.0f;
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          S[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + buf * G::STAGE + (u * KS + s) * 1024), Q[s], S[u], 0, 0, 0);
-      const float4 b0 = blocks[buf][c], b1 = blocks[buf][2 + c];
-      // tokens of this lane that its row does not see, where there are any
-      const bool masked = !(__all(b0.w != 0.0f && b1.w != 0.0f) && t0 >= all_lo && t0 + 64 <= all_hi);
-      uint32_t off = 0;
-      if (masked) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bool ok = (u ? b1.w : b0.w) != 0.0f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int tok = t0 + u * 32 + c * 16 + i;
-            const bool sees = ok & (tok >= rlo) & (tok < rhi);
-            off |= sees ? 0u : 1u << (u * 16 + i);
-            S[u][i] = sees ? S[u][i] : -INFINITY;
-          }
-        }
-      }
-      // s fk + lv, fk >= 0: the largest comes from the largest product
-      const float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
-      float mx = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float m = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) m = fmaxf(m, S[u][i]);
-        mx = fmaxf(mx, m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[u], lv[u]));
-      }
-      mx = other_half_max(mx);
-      if (__any(mx > M + kSlack)) {
-        const float mn = fmaxf(M, mx), alpha = exp2_fast(M - (mn == -INFINITY ? 0.0f : mn));
-        M = mn;
-        L *= alpha;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) O[d] *= alpha;
-      }
-      const float ms = M == -INFINITY ? 0.0f : M;
-      h8 P[2][2];
-      auto weights = [&](auto some) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const float o = lv[u] - ms;
-          float sum = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float p = exp2_fast(__builtin_fmaf(S[u][i], fk[u], o));
-            if constexpr (decltype(some)::value) p = off >> (u * 16 + i) & 1u ? 0.0f : p;
-            sum += p;
-            P[u][i >> 3][i & 7] = (_Float16)p;
-          }
-          L += sum == 0.0f ? 0.0f : sum * (u ? b1.z : b0.z);
-        }
-      };
-      if (masked) weights(std::true_type());
-      else weights(std::false_type());
+
+  // matrix phase of tile i: the second product of tile i - 1, the first of tile i
+  auto products = [&](int i, auto which) __attribute__((always_inline)) {
+    constexpr int b = decltype(which)::value;
+    if (busy) {
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + buf * G::STAGE + G::KEYS + d * 4096 + k * 1024),
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + (2 + (b ^ 1)) * G::KEYS + d * 4096 + k * 1024),
                                                          P[k >> 1][k & 1], O[d], 0, 0, 0);
     }
-    put(buf ^ 1);
-    __syncthreads();
+    busy = i < te && i * 64 < any_hi && i * 64 + 64 > any_lo;
+    if (busy) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          S[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + b * G::KEYS + (u * KS + s) * 1024), Q[s], S[u], 0, 0, 0);
+    }
   };
-  for (int tile = tb; tile < te; tile += 2) {
-    step(tile, std::integral_constant<int, 0>());
-    if (tile + 1 < te) step(tile + 1, std::integral_constant<int, 1>());
+  // vector phase: the weights of tile i
+  auto weigh = [&](int i, auto which) __attribute__((always_inline)) {
+    constexpr int b = decltype(which)::value;
+    if (!busy) return;
+    const int t0 = i * 64;
+    const float4 b0 = blocks[b][c], b1 = blocks[b][2 + c];
+    // tokens of this lane that its row does not see, where there are any
+    const bool masked = !(__all(b0.w != 0.0f && b1.w != 0.0f) && t0 >= all_lo && t0 + 64 <= all_hi);
+    uint32_t off = 0;
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bool ok = (u ? b1.w : b0.w) != 0.0f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int tok = t0 + u * 32 + c * 16 + j;
+          const bool sees = ok & (tok >= rlo) & (tok < rhi);
+          off |= sees ? 0u : 1u << (u * 16 + j);
+          S[u][j] = sees ? S[u][j] : -INFINITY;
+        }
+      }
+    }
+    // s fk + lv, fk >= 0: the largest comes from the largest product
+    const float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) m = fmaxf(m, S[u][j]);
+      mx = fmaxf(mx, m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[u], lv[u]));
+    }
+    mx = other_half_max(mx);
+    if (__any(mx > M + kSlack)) {
+      const float mn = fmaxf(M, mx), alpha = exp2_fast(M - (mn == -INFINITY ? 0.0f : mn));
+      M = mn;
+      L *= alpha;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] *= alpha;
+    }
+    const float ms = M == -INFINITY ? 0.0f : M;
+    auto weights = [&](auto some) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float o = lv[u] - ms;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          float p = exp2_fast(__builtin_fmaf(S[u][j], fk[u], o));
+          if constexpr (decltype(some)::value) p = off >> (u * 16 + j) & 1u ? 0.0f : p;
+          sum += p;
+          P[u][j >> 3][j & 7] = (_Float16)p;
+        }
+        L += sum == 0.0f ? 0.0f : sum * (u ? b1.z : b0.z);
+      }
+    };
+    if (masked) weights(std::true_type());
+    else weights(std::false_type());
+  };
+
+  if (tb < te) {
+    // 8 waves go as two groups half a step apart, one in its matrix phase while the
+    // other, on the same SIMDs, is in its vector phase: with all in step, the matrix
+    // cores stood idle during every softmax.  Group 1 is a phase behind, so it brings a
+    // tile ahead; a tile's last readers are two phases before its place is taken.
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    entries(tb, ent[0]);
+    entries(tb + 1, ent[1]);
+    load(tb, ent[0]);
+    bring(tb, even);  // (there are no values yet: those of tile tb, twice)
+    __syncthreads();
+    auto run = [&](auto group) __attribute__((always_inline)) {
+      constexpr int gr = decltype(group)::value;
+      auto both = [&](int i, auto which) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_setprio(1);
+        products(i, which);
+        __builtin_amdgcn_s_setprio(0);
+        if (W == 8) __syncthreads();
+        if (i < te) {
+          weigh(i, which);
+          bring(i + 1 + gr, std::integral_constant<int, (decltype(which)::value + 1 + gr) & 1>());
+          __syncthreads();
+        }
+      };
+      for (int i = tb; i <= te; i += 2) {
+        both(i, even);
+        if (i + 1 <= te) both(i + 1, odd);
+      }
+    };
+    if (W < 8 || wave < 4) {
+      run(even);
+      if (W == 8) __syncthreads();  // as many as the other group's
+    } else {
+      bring(tb + 1, odd);
+      __syncthreads();
+      run(odd);
+    }
   }
+  __syncthreads();
 
   L += __shfl_xor(L, 32);
   if (a.splits > 1) {
