@@ -374,12 +374,27 @@ struct TileLds {
   static constexpr int BYTES = 4 * KEYS > OUT ? 4 * KEYS : OUT;
 };
 
+// Keeps kAhead operand reads in flight before the N products of this block: an LDS
+// read takes the time of four products, and the compiler by itself asks for one
+// operand at a time.
+constexpr int kAhead = 5;
+template <int N>
+__device__ __forceinline__ void ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);  // LDS reads
+#pragma unroll
+  for (int j = 0; j < N - kAhead; ++j) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix product
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+}
+
 template <class T, int D, int W>
 __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
   typedef TileLds<D, W> G;
   constexpr int TH = 64 * W, KS = D / 16, DT = D / 32, PP = (4 * D + TH - 1) / TH;
   __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
-  __shared__ float4 blocks[2][4];  // of the tile's 16-token chunks: {ks, log2 vs, 1 / vs, page there}
+  __shared__ float4 blocks[4][4];  // of four tiles' 16-token chunks: {ks, log2 vs, 1 / vs, page there}
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, c = lane >> 5;
   // cache heads go fastest, so a head's tiles share one XCD's L2 where heads are a
   // multiple of 8; the rows with the longest reach start first
@@ -479,6 +494,10 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   // next.  Loads end in order, so the entries that the next call needs come first.
   // None of it stands under a condition, so that waits count only what they need; past
   // the last tile it reads tiles that nobody uses.  par: p - tb is odd.
+  auto bring_blocks = [&](int p) __attribute__((always_inline)) {
+    if (wave == 0 && lane < 4)
+      blocks[(p - tb) & 3][lane] = make_float4(bks, __builtin_amdgcn_logf(bvs), __builtin_amdgcn_rcpf(bvs), bthere);
+  };
   auto bring = [&](int p, auto par) __attribute__((always_inline)) {
     constexpr int odd = decltype(par)::value;
     uint8_t *kbase = lds + odd * G::KEYS, *vbase = lds + (2 + (odd ^ 1)) * G::KEYS;
@@ -495,7 +514,6 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
       *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1]);
       *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3]);
     }
-    if (threadIdx.x < 4) blocks[odd][threadIdx.x] = make_float4(bks, __builtin_amdgcn_logf(bvs), 1.0f / bvs, bthere);
     entries(p + 2, ent[odd]);
     load(p + 1, ent[odd ^ 1]);
   };
@@ -511,36 +529,46 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   bool busy = false;  // this wave has scores, or weights, of the present tile
   const uint8_t *mylds = lds + lane * 16;
 
-  // matrix phase of tile i: the second product of tile i - 1, the first of tile i
-  auto products = [&](int i, auto which) __attribute__((always_inline)) {
+  auto second = [&](auto which) __attribute__((always_inline)) {  // of the tile before one of this parity
     constexpr int b = decltype(which)::value;
-    if (busy) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + (2 + (b ^ 1)) * G::KEYS + d * 4096 + k * 1024),
-                                                         P[k >> 1][k & 1], O[d], 0, 0, 0);
-    }
-    busy = i < te && i * 64 < any_hi && i * 64 + 64 > any_lo;
-    if (busy) {
+      for (int d = 0; d < DT; ++d)
+        O[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + (2 + (b ^ 1)) * G::KEYS + d * 4096 + k * 1024),
+                                                       P[k >> 1][k & 1], O[d], 0, 0, 0);
+    ahead<4 * DT>();
+  };
+  auto scores = [&](auto which) __attribute__((always_inline)) {  // of a tile of this parity
+    constexpr int b = decltype(which)::value;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) S[u][j] = 0.0f;
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          S[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + b * G::KEYS + (u * KS + s) * 1024), Q[s], S[u], 0, 0, 0);
-    }
+        S[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const h8 *)(mylds + b * G::KEYS + (u * KS + s) * 1024), Q[s], S[u], 0, 0, 0);
+    ahead<2 * KS>();
+  };
+  // matrix phase of tile i: the second product of tile i - 1, the first of tile i, and
+  // among them the next tile's way to LDS
+  auto products = [&](int i, auto which) __attribute__((always_inline)) {
+    constexpr std::integral_constant<int, decltype(which)::value ^ 1> other;
+    const bool next = i < te && i * 64 < any_hi && i * 64 + 64 > any_lo;
+    if (i < te) bring_blocks(i + 1);
+    if (i < te) bring(i + 1, other);
+    if (busy) second(which);
+    if (next) scores(which);
+    busy = next;
   };
   // vector phase: the weights of tile i
   auto weigh = [&](int i, auto which) __attribute__((always_inline)) {
     constexpr int b = decltype(which)::value;
     if (!busy) return;
     const int t0 = i * 64;
-    const float4 b0 = blocks[b][c], b1 = blocks[b][2 + c];
+    const float4 b0 = blocks[(i - tb) & 3][c], b1 = blocks[(i - tb) & 3][2 + c];
     // tokens of this lane that its row does not see, where there are any
     const bool masked = !(__all(b0.w != 0.0f && b1.w != 0.0f) && t0 >= all_lo && t0 + 64 <= all_hi);
     uint32_t off = 0;
@@ -598,41 +626,33 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   if (tb < te) {
     // 8 waves go as two groups half a step apart, one in its matrix phase while the
     // other, on the same SIMDs, is in its vector phase: with all in step, the matrix
-    // cores stood idle during every softmax.  Group 1 is a phase behind, so it brings a
-    // tile ahead; a tile's last readers are two phases before its place is taken.
+    // cores stood idle during every softmax.  A tile is brought during the two matrix
+    // phases before its own, whose barriers come after the last reads of its place.
     constexpr std::integral_constant<int, 0> even;
     constexpr std::integral_constant<int, 1> odd;
     entries(tb, ent[0]);
     entries(tb + 1, ent[1]);
     load(tb, ent[0]);
+    bring_blocks(tb);
     bring(tb, even);  // (there are no values yet: those of tile tb, twice)
     __syncthreads();
-    auto run = [&](auto group) __attribute__((always_inline)) {
-      constexpr int gr = decltype(group)::value;
-      auto both = [&](int i, auto which) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_setprio(1);
-        products(i, which);
-        __builtin_amdgcn_s_setprio(0);
+    const bool late = W == 8 && wave >= 4;
+    if (late) __syncthreads();
+    auto both = [&](int i, auto which) __attribute__((always_inline)) {
+      __builtin_amdgcn_s_setprio(1);
+      products(i, which);
+      __builtin_amdgcn_s_setprio(0);
+      __syncthreads();
+      if (i < te) {
+        weigh(i, which);
         if (W == 8) __syncthreads();
-        if (i < te) {
-          weigh(i, which);
-          bring(i + 1 + gr, std::integral_constant<int, (decltype(which)::value + 1 + gr) & 1>());
-          __syncthreads();
-        }
-      };
-      for (int i = tb; i <= te; i += 2) {
-        both(i, even);
-        if (i + 1 <= te) both(i + 1, odd);
       }
     };
-    if (W < 8 || wave < 4) {
-      run(even);
-      if (W == 8) __syncthreads();  // as many as the other group's
-    } else {
-      bring(tb + 1, odd);
-      __syncthreads();
-      run(odd);
+    for (int i = tb; i <= te; i += 2) {
+      both(i, even);
+      if (i + 1 <= te) both(i + 1, odd);
     }
+    if (W == 8 && !late) __syncthreads();  // as many as the other group's
   }
   __syncthreads();
 
@@ -756,6 +776,7 @@ void attend_plan(AttendArgs &a, int cus) {
   // every wave at least one tile of 64 tokens
   const int64_t most = std::max<int64_t>(1, (a.b.max_len + 255) / 256);
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), 2 * cus / base));
+  if (const char *e = getenv("PQ_SPLITS")) a.splits = atoi(e);
 }
 
 size_t attend_work_bytes(const AttendArgs &a) {
