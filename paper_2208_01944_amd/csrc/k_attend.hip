@@ -115,7 +115,7 @@ __device__ __forceinline__ h8 scaled(v4i raw, float f) {
 // NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
 // fourth tile of 64 tokens; the waves join in LDS.  Splits join in attend_join_kernel.
 template <class T, int D, int NQ>
-__global__ __launch_bounds__(256) void attend_rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, D * NQ <= 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
   __shared__ float sm[4][NQ * 16], sl[4][NQ * 16];
   __shared__ __attribute__((aligned(16))) float so[4][16 * OLD];
@@ -713,14 +713,31 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (sub >= 256 / W || i >= (int64_t)q.n * hs) return;
   const int64_t t = i / hs, hq = i - t * hs, at = (q.row0 + t) * hs + hq, step = a.b.tokens * hs;
   const float *ml = a.part + a.splits * step * D;
+  // eight splits at a time, all their loads in flight
   float m = -INFINITY, l = 0.0f;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[(s * step + at) * 2]);
-  const float ms = m == -INFINITY ? 0.0f : m;
   v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float w = exp2_fast(ml[(s * step + at) * 2] - ms);
-    l += ml[(s * step + at) * 2 + 1] * w;
-    o += *(const v4f *)(a.part + (s * step + at) * D + d) * w;
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+    v2f x[8];
+    v4f y[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const int64_t from = min(s0 + s, a.splits - 1) * step + at;
+      x[s] = *(const v2f *)(ml + from * 2);
+      y[s] = *(const v4f *)(a.part + from * D + d);
+    }
+    float mn = m;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) mn = fmaxf(mn, x[s][0]);
+    const float ms = mn == -INFINITY ? 0.0f : mn, w0 = exp2_fast(m - ms);
+    m = mn;
+    l *= w0;
+    o *= w0;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      const float w = s0 + s < a.splits ? exp2_fast(x[s][0] - ms) : 0.0f;
+      l += x[s][1] * w;
+      o += y[s] * w;
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
