@@ -21,12 +21,13 @@ struct AttendArgs {
   int32_t group;                             // query heads of a cache head
   int32_t causal, window;
   float scale;                               // of the scores, times log2(e)
+  int32_t block;                             // rows of a workgroup
   int32_t splits;                            // parts that a request's tokens are cut into
   float *part;                               // their results (attend_work_bytes)
 };
 
-// How many parts, and the device memory for them.
-void attend_plan(AttendArgs &a, int cus);
+// Chooses kernel and parts (false: a grid past 2^31), and the device memory for the parts.
+bool attend_plan(AttendArgs &a, int cus);
 size_t attend_work_bytes(const AttendArgs &a);
 hipError_t launch_attend(const AttendArgs &a, int type, hipStream_t s);
 

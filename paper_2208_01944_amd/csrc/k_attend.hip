@@ -24,7 +24,6 @@
 // stored channel by channel, is read 16 tokens at a time.
 #include <algorithm>
 #include <type_traits>
-#include <stdlib.h>
 
 #include "cache.h"
 
@@ -75,18 +74,10 @@ __device__ __forceinline__ RowScale row_scale(uint32_t mag) {
   return {e == 255 ? 0.0f : __uint_as_float((uint32_t)(254 - b) << 23), __uint_as_float((uint32_t)b << 23)};
 }
 
-// 8 n consecutive elements at p (16-byte loads where vec), two in a word.
-template <int N>
-__device__ __forceinline__ void load_words(const uint16_t *p, bool vec, v4i *raw) {
-  if (vec) {
+// 8 consecutive elements at p, which is aligned to elements only, two in a word.
+__device__ __forceinline__ void load_words(const uint16_t *p, v4i &raw) {
 #pragma unroll
-    for (int s = 0; s < N; ++s) raw[s] = ((const v4i *)p)[s];
-  } else {
-#pragma unroll
-    for (int s = 0; s < N; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) raw[s][i] = (int)((uint32_t)p[s * 8 + 2 * i] | (uint32_t)p[s * 8 + 2 * i + 1] << 16);
-  }
+  for (int i = 0; i < 4; ++i) raw[i] = (int)((uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16);
 }
 template <class T>
 __device__ __forceinline__ float low(int w) { return T::get((uint16_t)((uint32_t)w & 0xffffu)); }
@@ -115,8 +106,9 @@ __device__ __forceinline__ h8 scaled(v4i raw, float f) {
 // NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
 // fourth tile of 64 tokens; the waves join in LDS.  Splits join in attend_join_kernel.
 template <class T, int D, int NQ>
-__global__ __launch_bounds__(256, D * NQ <= 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
+__global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
+  constexpr int CH = D % 64 == 0 ? 16 : 8;  // consecutive channels of a key that a lane loads at once
   __shared__ float sm[4][NQ * 16], sl[4][NQ * 16];
   __shared__ __attribute__((aligned(16))) float so[4][16 * OLD];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4;
@@ -135,8 +127,8 @@ __global__ __launch_bounds__(256, D * NQ <= 256 ? 2 : 1) void attend_rows_kernel
   const int per = (ntiles + a.splits - 1) / a.splits;
   const int tb = tile0 + min(ntiles, split * per), te = tile0 + min(ntiles, (split + 1) * per);
 
-  h8 Q[NQ][KS];
-  float f[NQ];
+  // the rows' elements are on their way while the tokens' pages are looked up
+  v4i raw[NQ][KS];
   int rlo[NQ], rhi[NQ];
   const bool vec = (((uintptr_t)a.q | (uintptr_t)(a.q_row * 2) | (uintptr_t)(a.q_head * 2)) & 15u) == 0;
 #pragma unroll
@@ -144,19 +136,19 @@ __global__ __launch_bounds__(256, D * NQ <= 256 ? 2 : 1) void attend_rows_kernel
     const int row = first + n * 16 + col;
     const bool live = row < rows;
     const int t = live ? row / a.group : 0, g = live ? row - t * a.group : 0;
-    // this lane's channels c D / 4 .. of row lane % 16 (of the first row past the last)
-    v4i raw[KS];
-    load_words<KS>(a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * (D / 4), vec, raw);
-    uint32_t mag = largest<T, KS>(raw);
-    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 16));
-    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
-    const RowScale rs = row_scale(mag);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) Q[n][s] = scaled<T>(raw[s], rs.in);
-    f[n] = rs.out * a.scale;
     const Reach s = reach_of(a, q, t);
     rlo[n] = s.lo;
     rhi[n] = live ? s.hi : 0;
+    // this lane's channels of row lane % 16 (of the first row past the last): of every
+    // 64 (32 where 64 do not divide the head) the 16 (8) from 16 c (8 c) on, as the keys'
+    const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * CH;
+    if (vec) {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) raw[n][s] = *(const v4i *)(p + s * 8 / CH * 4 * CH + s * 8 % CH);
+    } else {
+#pragma unroll
+      for (int s = 0; s < KS; ++s) load_words(p + s * 8 / CH * 4 * CH + s * 8 % CH, raw[n][s]);
+    }
   }
   v4f O[NQ][DT];
   float M[NQ], L[NQ];
@@ -184,23 +176,23 @@ __global__ __launch_bounds__(256, D * NQ <= 256 ? 2 : 1) void attend_rows_kernel
     const int kt = tile * 64 + kc, vt = tile * 64 + vc;
     const bool kok = ((uint32_t)kpage < (uint32_t)cv.pages) & (kt < hi);
     vthere = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
-    const int8_t *kb = cv.k + (((int64_t)(kok ? kpage : 0) * heads + h) * cv.page + (kt & pm) + (col & 3)) * D + c * (D / 4);
+    const int8_t *kb = cv.k + (((int64_t)(kok ? kpage : 0) * heads + h) * cv.page + (kt & pm) + (col & 3)) * D + c * CH;
     const int64_t sc = (int64_t)(vthere ? vpage : 0) * heads + h;
     ks = cv.ks[sc];
     vs = cv.vs[sc];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if constexpr (D % 64 == 0) {
+      if constexpr (CH == 16) {  // (four lanes then share 64 bytes of a row: half the cache accesses of 16 D / 4 apart)
 #pragma unroll
         for (int w = 0; w < D / 64; ++w) {
-          const v4i x = *(const v4i *)(kb + j * 4 * D + w * 16);
+          const v4i x = *(const v4i *)(kb + j * 4 * D + w * 64);
 #pragma unroll
           for (int i = 0; i < 4; ++i) kx[j][4 * w + i] = (uint32_t)x[i];
         }
       } else {
 #pragma unroll
         for (int w = 0; w < D / 32; ++w) {
-          const v2i x = *(const v2i *)(kb + j * 4 * D + w * 8);
+          const v2i x = *(const v2i *)(kb + j * 4 * D + w * 32);
           kx[j][2 * w] = (uint32_t)x[0];
           kx[j][2 * w + 1] = (uint32_t)x[1];
         }
@@ -224,6 +216,18 @@ __global__ __launch_bounds__(256, D * NQ <= 256 ? 2 : 1) void attend_rows_kernel
     vpage = entry((tb + wave) * 64 + vc);
     load_k(tb + wave);
     load_v(tb + wave);
+  }
+  h8 Q[NQ][KS];
+  float f[NQ];
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    uint32_t mag = largest<T, KS>(raw[n]);
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 16));
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
+    const RowScale rs = row_scale(mag);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) Q[n][s] = scaled<T>(raw[n][s], rs.in);
+    f[n] = rs.out * a.scale;
   }
   auto step = [&](int tile, auto last) __attribute__((always_inline)) {
     constexpr bool more = !decltype(last)::value;
@@ -367,10 +371,10 @@ __device__ __forceinline__ float other_half_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int D, int W>
+template <int D>
 struct TileLds {
   static constexpr int KEYS = 64 * D * 2;            // bytes of a tile's keys, and of its values
-  static constexpr int OUT = 32 * W * (D * 2 + 16);  // the epilogue's rows
+  static constexpr int OUT = 128 * (D * 2 + 16);  // the epilogue's rows
   static constexpr int BYTES = 4 * KEYS > OUT ? 4 * KEYS : OUT;
 };
 
@@ -389,10 +393,10 @@ __device__ __forceinline__ void ahead() {
   __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
 
-template <class T, int D, int W>
-__global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
-  typedef TileLds<D, W> G;
-  constexpr int TH = 64 * W, KS = D / 16, DT = D / 32, PP = (4 * D + TH - 1) / TH;
+template <class T, int D>
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
+  typedef TileLds<D> G;
+  constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + 255) / 256;
   __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
   __shared__ float4 blocks[4][4];  // of four tiles' 16-token chunks: {ks, log2 vs, 1 / vs, page there}
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, c = lane >> 5;
@@ -403,9 +407,9 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   const int h = combo % heads, r = (combo / heads + rest) % a.b.requests, split = rest % a.splits, rt = row_tiles - 1 - rest / a.splits;
   const CacheView &cv = a.c;
   const Request q = request_of(a.b, r, cv.shift);
-  const int rows = q.n * a.group, first = rt * 32 * W;
+  const int rows = q.n * a.group, first = rt * ROWS;
   if (first >= rows) return;
-  const int last = min(rows, first + 32 * W) - 1;
+  const int last = min(rows, first + ROWS) - 1;
   const Reach rf = reach_of(a, q, first / a.group), rl = reach_of(a, q, last / a.group);
   const int hi = rl.hi;
   const int tile0 = rf.lo >> 6, ntiles = hi > rf.lo ? ((hi + 63) >> 6) - tile0 : 0;
@@ -434,7 +438,7 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
       for (int s = 0; s < KS; ++s) raw[s] = *(const v4i *)(p + s * 16);
     } else {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) load_words<1>(p + s * 16, false, &raw[s]);
+      for (int s = 0; s < KS; ++s) load_words(p + s * 16, raw[s]);
     }
     uint32_t mag = largest<T, KS>(raw);
     mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
@@ -455,10 +459,10 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   // tokens of a value channel of tile p - 1.
   struct Piece { int tok, s, kr, d, vt; };  // key's token, 16 channels, matrix row; value's channel, first token
   auto piece = [&](int i) __attribute__((always_inline)) {
-    const int p = threadIdx.x + i * TH, j = p & 7, s = p / 8 % KS, gu = p / (8 * KS), g = gu & 3, u = gu >> 2;
+    const int p = threadIdx.x + i * 256, j = p & 7, s = p / 8 % KS, gu = p / (8 * KS), g = gu & 3, u = gu >> 2;
     return Piece{u * 32 + (j >> 2) * 16 + g * 4 + (j & 3), s, u * 32 + g * 8 + j, (p >> 6) * 16 + (p & 15), (p >> 4 & 3) * 16};
   };
-  auto none = [&](int i) __attribute__((always_inline)) { return 4 * D % TH && (int)threadIdx.x + i * TH >= 4 * D; };
+  auto none = [&](int i) __attribute__((always_inline)) { return 4 * D % 256 && (int)threadIdx.x + i * 256 >= 4 * D; };
   // Table entries go through two sets of registers by the tile's parity (a copy from
   // one to the other would wait for them, and so for every load before them).
   struct Entries { int k[PP], v[PP], b; } ent[2];
@@ -624,10 +628,6 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
   };
 
   if (tb < te) {
-    // 8 waves go as two groups half a step apart, one in its matrix phase while the
-    // other, on the same SIMDs, is in its vector phase: with all in step, the matrix
-    // cores stood idle during every softmax.  A tile is brought during the two matrix
-    // phases before its own, whose barriers come after the last reads of its place.
     constexpr std::integral_constant<int, 0> even;
     constexpr std::integral_constant<int, 1> odd;
     entries(tb, ent[0]);
@@ -636,23 +636,19 @@ __global__ __launch_bounds__(64 * W, D > 128 ? 1 : 2) void attend_tile_kernel(At
     bring_blocks(tb);
     bring(tb, even);  // (there are no values yet: those of tile tb, twice)
     __syncthreads();
-    const bool late = W == 8 && wave >= 4;
-    if (late) __syncthreads();
+    // One barrier a step: what a step brings to LDS is read in the next, and takes the
+    // place of what was read in the step before.
     auto both = [&](int i, auto which) __attribute__((always_inline)) {
-      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_s_setprio(1);  // before the CU's other workgroup in its softmax
       products(i, which);
       __builtin_amdgcn_s_setprio(0);
       __syncthreads();
-      if (i < te) {
-        weigh(i, which);
-        if (W == 8) __syncthreads();
-      }
+      if (i < te) weigh(i, which);
     };
     for (int i = tb; i <= te; i += 2) {
       both(i, even);
       if (i + 1 <= te) both(i + 1, odd);
     }
-    if (W == 8 && !late) __syncthreads();  // as many as the other group's
   }
   __syncthreads();
 
@@ -745,28 +741,25 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store4<T>(dst, v, (((uintptr_t)a.out | (uintptr_t)(a.out_row * 2) | (uintptr_t)(a.out_head * 2)) & 7u) == 0);
 }
 
-// Rows of a workgroup: 16, 32 or 64 on attend_rows_kernel, 32 a wave on attend_tile_kernel.
-int block_rows(const AttendArgs &a) {
-  const int64_t rows = (int64_t)a.b.max_new * a.group;
-  static const char *force = getenv("PQ_ROWS");
-  if (force) return atoi(force);
-  if (rows <= 32) return rows <= 16 ? 16 : 32;
-  return rows <= 128 || a.c.dim == 256 ? 128 : 256;
+// Rows of a workgroup: 16 or 32 on attend_rows_kernel, 128 on attend_tile_kernel.
+// While the small blocks are at most 3 for each CU, their many waves over the
+// tokens end sooner than the tile kernel's long chain of steps, although each
+// block converts its codes itself: 4 requests, 8 heads, group 4, 2048 tokens, 64 /
+// 128 / 256 new ones: 30 / 44 / 79 us against 64 / 66 / 70.
+int block_rows(const AttendArgs &a, int cus) {
+  const int64_t rows = (int64_t)a.b.max_new * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
+  return (rows + small - 1) / small * a.c.heads * a.b.requests <= 3 * cus ? (int)small : 128;
 }
 
 template <class T, int D>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
-  const int br = block_rows(a);
-  const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + br - 1) / br;
-  if (br >= 128) {
-    const unsigned g = (unsigned)(rt * a.splits * a.c.heads * a.b.requests);
-    if (br == 128) attend_tile_kernel<T, D, 4><<<g, 256, 0, s>>>(a, (int)rt);
-    else if constexpr (D < 256) attend_tile_kernel<T, D, 8><<<g, 512, 0, s>>>(a, (int)rt);
+  const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
+  if (a.block == 128) {
+    attend_tile_kernel<T, D><<<(unsigned)(rt * a.splits * a.c.heads * a.b.requests), 256, 0, s>>>(a, (int)rt);
   } else {
     const dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
-    if (br == 16) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
-    else if (br == 32) attend_rows_kernel<T, D, 2><<<g, 256, 0, s>>>(a);
-    else if constexpr (D < 256) attend_rows_kernel<T, D, 4><<<g, 256, 0, s>>>(a);
+    if (a.block == 16) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
+    else if constexpr (D < 256) attend_rows_kernel<T, D, 2><<<g, 256, 0, s>>>(a);
   }
   if (a.splits > 1) {
     const int64_t per = 256 / (D / 4), n = (int64_t)a.b.max_new * a.c.heads * a.group;
@@ -787,13 +780,16 @@ hipError_t launch_attend_t(const AttendArgs &a, hipStream_t s) {
 
 }  // namespace
 
-void attend_plan(AttendArgs &a, int cus) {
-  const int64_t rows = (int64_t)a.b.max_new * a.group, nq = block_rows(a);
-  const int64_t base = std::max<int64_t>(1, (rows + nq - 1) / nq * a.c.heads * a.b.requests);
-  // every wave at least one tile of 64 tokens
-  const int64_t most = std::max<int64_t>(1, (a.b.max_len + 255) / 256);
-  a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), 2 * cus / base));
-  if (const char *e = getenv("PQ_SPLITS")) a.splits = atoi(e);
+bool attend_plan(AttendArgs &a, int cus) {
+  a.block = block_rows(a, cus);
+  const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
+  const int64_t base = std::max<int64_t>(1, rt * a.c.heads * a.b.requests);
+  // Parts of a request's tokens, each at least a tile for every wave: until two
+  // workgroups stand on every CU (one of 32 rows: its waves hold twice the
+  // accumulators; 4 requests, 5 tokens, window 8191: 23 us in 8 parts, 26 in 16).
+  const int64_t most = std::max<int64_t>(1, (a.b.max_len + 255) / 256), want = (a.block == 32 ? 1 : 2) * cus;
+  a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), want / base));
+  return base * a.splits < (int64_t)1 << 31;
 }
 
 size_t attend_work_bytes(const AttendArgs &a) {

@@ -225,6 +225,10 @@ palq_status palq_linear_run(palq_ctx *ctx, const palq_linear *lin, const void *x
   LinearArgs a{(int8_t *)work, lin->w, (float *)(work + padded * lin->kp), lin->w_scale, lin->bias, y, rows, y_ld,
                lin->n_out, lin->kp};
   hipError_t e;
+  if (x_type != PALQ_I8 && linear_one(rows, lin->kp)) {
+    e = launch_linear_one(a, x, x_type, x_ld, lin->n_in, y_type, ctx->stream);
+    return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "linear");
+  }
   if (x_type == PALQ_I8) {
     e = launch_slabs((const int8_t *)x, rows, up(rows, 16), lin->n_in, x_ld, lin->kp, (int8_t *)work, ctx->stream);
     a.x_scale = x_scale;
@@ -309,8 +313,9 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
   if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0) return PALQ_OK;
   hipSetDevice(ctx->device);
   AttendArgs a{view_of(cache), view_of(batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
-               group, causal, window, scale * 1.44269504088896340736f, 1, nullptr};
-  attend_plan(a, ctx->cus);
+               group, causal, window, scale * 1.44269504088896340736f, 0, 1, nullptr};
+  if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
+  if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^31 or more workgroups");
   if (const size_t need = attend_work_bytes(a)) {
     a.part = (float *)workspace(ctx, need);
     if (!a.part) return fail(ctx, PALQ_ERR_NOMEM, "attention: workspace (in a capture: run the shape once before)");

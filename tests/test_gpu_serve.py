@@ -81,7 +81,8 @@ def check_linear(got, q, s, w, ws, b, y_type):
 @pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("f16", "f32"), ("f32", "f16"), ("i8", "bf16"), ("f32", "f32"), ("i8", "f32")])
 @pytest.mark.parametrize("rows,n_in,n_out", [(1, 1, 1), (1, 64, 16), (1, 4096, 256), (2, 100, 33), (15, 129, 17), (16, 256, 64),
                                              (17, 300, 100), (33, 127, 130), (50, 640, 257), (64, 192, 320), (65, 1000, 1000),
-                                             (129, 65, 255), (257, 384, 513), (300, 2047, 258), (520, 130, 1030)])
+                                             (129, 65, 255), (257, 384, 513), (300, 2047, 258), (520, 130, 1030), (8, 8192, 40), (9, 8192, 40),
+                                             (3, 5000, 20), (1, 70000, 18), (200, 1500, 700), (1100, 260, 300)])
 def test_linear(palq, x_type, y_type, rows, n_in, n_out):
     import torch
     from paper_2208_01944_amd import palq as P
