@@ -47,10 +47,14 @@ struct NewKv {
   int64_t k_row, k_head, v_row, v_head;  // strides in elements; a row's channels are consecutive
 };
 
-template <class T>
+// A thread's item: 4 tokens x 8 channels, neighbouring lanes neighbouring channels;
+// NI items a thread hold a whole block in registers, so new values are read once.
+// Values are turned (a word of 4 tokens for each channel) through LDS.
+template <class T, int NI>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchView b, NewKv x) {
   typedef typename T::raw R;
   __shared__ uint32_t part[4];
+  __shared__ uint32_t turned[NI * 2048 + 256];  // [dim][page / 4 + 1] words
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
   const Request q = request_of(b, r, c.shift);
@@ -60,26 +64,52 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   if (lo >= hi) return;
   const int pid = page_of(c, b, r, block);
   if (pid < 0) return;
-  const int kept = lo - t0, n = hi - lo, D = c.dim;
+  const int kept = lo - t0, end = hi - t0, D = c.dim, groups = D / 8, items = c.page / 4 * groups;
   const R *src = (const R *)(values ? x.v : x.k);
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
-  src += (q.row0 + (lo - (q.len - q.n))) * row + h * head;  // row of token lo
-  const bool vec = (((uintptr_t)src | (uintptr_t)(row * sizeof(R))) & 15u) == 0;
-
-  // largest magnitude of the new values
-  uint32_t mag = 0;
-  const int pd = D / 16;
-  for (int p = threadIdx.x; p < n * pd; p += 256) {
-    float v[16];
-    load16<T>(src + (int64_t)(p / pd) * row + p % pd * 16, 16, vec, v);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) mag = max(mag, mag_bits(v[i]));
-  }
-  mag = wave_max(mag);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mag;
+  src += (q.row0 + (t0 - (q.len - q.n))) * row + h * head;  // row of token t0 (there may be none)
+  const bool vec = (((uintptr_t)(values ? x.v : x.k) | (uintptr_t)(row * (int64_t)sizeof(R)) | (uintptr_t)(head * (int64_t)sizeof(R))) & 15u) == 0;
   const int64_t ph = (int64_t)pid * c.heads + h;
   float *scale = (values ? c.vs : c.ks) + ph;
   const float had = kept ? *scale : 0.0f;
+
+  float v[NI][4][8];
+  uint32_t mag = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int p = threadIdx.x + i * 256, tq = p / groups * 4, ch = p % groups * 8;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const bool here = p < items && tq + t >= kept && tq + t < end;
+      const R *from = src + (int64_t)(tq + t) * row + ch;
+      if (here && vec) {
+        if constexpr (sizeof(R) == 4) {
+          const v4f a = ((const v4f *)from)[0], e = ((const v4f *)from)[1];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[i][t][j] = a[j];
+            v[i][t][4 + j] = e[j];
+          }
+        } else {
+          const v4i a = *(const v4i *)from;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[i][t][2 * j] = T::get((uint16_t)((uint32_t)a[j] & 0xffffu));
+            v[i][t][2 * j + 1] = T::get((uint16_t)((uint32_t)a[j] >> 16));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][t][j] = here ? T::get(from[j]) : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mag = max(mag, mag_bits(v[i][t][j]));
+  }
+  mag = wave_max(mag);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = mag;
   __syncthreads();
   mag = max(max(part[0], part[1]), max(part[2], part[3]));
   float s = scale_of(mag);
@@ -88,35 +118,58 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   const bool bad = !(s == s), grown = kept && !bad && s > had;
   if (threadIdx.x == 0) *scale = s;
   int8_t *dst = (values ? c.v : c.k) + ph * c.page * D;
-  if (!values) {
-    for (int p = threadIdx.x; p < n * pd; p += 256) {
-      float v[16];
-      load16<T>(src + (int64_t)(p / pd) * row + p % pd * 16, 16, vec, v);
-      *(v4i *)(dst + (int64_t)(kept + p / pd) * D + p % pd * 16) = bad ? v4i{0, 0, 0, 0} : quantize16(v, inv);
-    }
-    if (grown)
-      for (int p = threadIdx.x; p < kept * pd; p += 256) ((v4i *)dst)[p] = rescale16(((const v4i *)dst)[p], ratio);
-  } else {
-    // a piece: 16 tokens of one channel; neighbouring lanes take neighbouring channels
-    const int c0 = grown ? 0 : kept >> 4, pieces = ((hi - t0 + 15) >> 4) - c0;
-    for (int p = threadIdx.x; p < pieces * D; p += 256) {
-      const int d = p % D, at = (c0 + p / D) * 16;
-      v4i *piece = (v4i *)(dst + (int64_t)d * c.page + at);
-      v4i o = {0, 0, 0, 0};
-      if (at < kept) {
-        o = *piece;
-        if (grown) o = rescale16(o, ratio);
-      }
+  const int words = c.page / 4 + 1;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int t = at + i - kept;
-        if (t >= 0) {
-          const int code = t < n && !bad ? code_of(T::get(src[(int64_t)t * row + d]), inv) : 0;
-          o[i >> 2] = (int)(((uint32_t)o[i >> 2] & ~(0xffu << (8 * (i & 3)))) | ((uint32_t)code & 0xffu) << (8 * (i & 3)));
-        }
+  for (int i = 0; i < NI; ++i) {
+    const int p = threadIdx.x + i * 256, tq = p / groups * 4, ch = p % groups * 8;
+    if (p >= items || tq + 4 <= kept || tq >= end) continue;
+    uint32_t w[4][2];  // codes of a token's 8 channels
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        w[t][q] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[t][q] |= bad ? 0u : ((uint32_t)code_of(v[i][t][4 * q + j], inv) & 0xffu) << (8 * j);
       }
-      *piece = o;
+    if (!values) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (tq + t >= kept && tq + t < end) *(v2i *)(dst + (tq + t) * D + ch) = v2i{(int)w[t][0], (int)w[t][1]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {  // byte j of four tokens
+        const int q = j >> 2, at = 8 * (j & 3);
+        turned[(ch + j) * words + tq / 4] = (w[0][q] >> at & 0xffu) | (w[1][q] >> at & 0xffu) << 8 | (w[2][q] >> at & 0xffu) << 16 |
+                                            (w[3][q] >> at & 0xffu) << 24;
+      }
     }
+  }
+  if (!values) {
+    if (grown)
+      for (int p = threadIdx.x; p < kept * (D / 16); p += 256) ((v4i *)dst)[p] = rescale16(((const v4i *)dst)[p], ratio);
+    return;
+  }
+  __syncthreads();
+  // a piece: 16 tokens of one channel; where old ones are among them, or all are and the
+  // scale grew, what is there comes first
+  const int c0 = grown ? 0 : kept >> 4, pieces = ((end + 15) >> 4) - c0;
+  for (int p = threadIdx.x; p < pieces * D; p += 256) {
+    const int d = p / pieces, at = (c0 + p % pieces) * 16;
+    v4i *piece = (v4i *)(dst + d * c.page + at);
+    v4i o = {0, 0, 0, 0};
+    if (at < kept) {
+      o = *piece;
+      if (grown) o = rescale16(o, ratio);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int t = at + 4 * j;
+      if (t + 4 <= kept || t >= end) continue;
+      const uint32_t fresh = t >= kept ? 0xffffffffu : 0xffffffffu << (8 * (kept - t));
+      o[j] = (int)(((uint32_t)o[j] & ~fresh) | (turned[d * words + (t >> 2)] & fresh));
+    }
+    *piece = o;
   }
 }
 
@@ -142,25 +195,42 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
   R *dst = (R *)(values ? x.v : x.k) + (q.row0 + (lo - (q.len - q.n))) * row + h * head;
   const bool al = (((uintptr_t)dst | (uintptr_t)(row * sizeof(R))) & (4 * sizeof(R) - 1)) == 0;
+  // several pieces' loads in flight before the first store
   if (!values) {
-    const int quads = D / 4;
-    for (int p = threadIdx.x; p < (hi - lo) * quads; p += 256) {
-      const int t = p / quads, d = p % quads * 4;
-      const uint32_t w = *(const uint32_t *)(src + (int64_t)(lo - t0 + t) * D + d);
-      float v[4];
+    const int quads = D / 4, all = (hi - lo) * quads;
+    const uint32_t *from = (const uint32_t *)(src + (int64_t)(lo - t0) * D);
+    for (int p0 = threadIdx.x; p0 < all; p0 += 256 * 8) {
+      uint32_t w[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(w >> (8 * i)) * s;
-      store4<T>(dst + (int64_t)t * row + d, v, al);
+      for (int i = 0; i < 8; ++i) w[i] = from[min(p0 + i * 256, all - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int p = p0 + i * 256, t = p / quads, d = p % quads * 4;
+        if (p >= all) break;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = (float)(int8_t)(w[i] >> (8 * j)) * s;
+        store4<T>(dst + (int64_t)t * row + d, v, al);
+      }
     }
   } else {
-    const int c0 = (lo - t0) >> 4, pieces = ((hi - t0 + 15) >> 4) - c0;
-    for (int p = threadIdx.x; p < pieces * D; p += 256) {
-      const int d = p % D, at = (c0 + p / D) * 16;
-      const v4i o = *(const v4i *)(src + (int64_t)d * c.page + at);
+    const int c0 = (lo - t0) >> 4, all = (((hi - t0 + 15) >> 4) - c0) * D;
+    for (int p0 = threadIdx.x; p0 < all; p0 += 256 * 2) {
+      v4i o[2];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int t = t0 + at + i;
-        if (t >= lo && t < hi) dst[(int64_t)(t - lo) * row + d] = T::put((float)(int8_t)((uint32_t)o[i >> 2] >> (8 * (i & 3))) * s);
+      for (int i = 0; i < 2; ++i) {
+        const int p = min(p0 + i * 256, all - 1);
+        o[i] = *(const v4i *)(src + (int64_t)(p % D) * c.page + (c0 + p / D) * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int p = p0 + i * 256, d = p % D, at = (c0 + p / D) * 16;
+        if (p >= all) break;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int t = t0 + at + j;
+          if (t >= lo && t < hi) dst[(int64_t)(t - lo) * row + d] = T::put((float)(int8_t)((uint32_t)o[i][j >> 2] >> (8 * (j & 3))) * s);
+        }
       }
     }
   }
@@ -172,15 +242,24 @@ unsigned blocks_of(const CacheView &c, const BatchView &b) {
   return (unsigned)std::min<int64_t>((n + c.page - 2) / c.page + 1, b.max_pages);
 }
 
+// Items of a thread: a block of page x dim elements, 32 an item, 256 threads.
+template <class T>
+void launch_append_t(dim3 g, const CacheView &c, const BatchView &b, const NewKv &x, hipStream_t s) {
+  const int n = c.page * c.dim / 8192;
+  if (n <= 1) cache_append_kernel<T, 1><<<g, 256, 0, s>>>(c, b, x);
+  else if (n <= 2) cache_append_kernel<T, 2><<<g, 256, 0, s>>>(c, b, x);
+  else cache_append_kernel<T, 4><<<g, 256, 0, s>>>(c, b, x);
+}
+
 }  // namespace
 
 hipError_t launch_cache_append(const CacheView &c, const BatchView &b, const void *k, const void *v, int type,
                                const int64_t *stride, hipStream_t s) {
   const dim3 g(blocks_of(c, b), (unsigned)c.heads, (unsigned)b.requests * 2);
   const NewKv x{k, v, stride[0], stride[1], stride[2], stride[3]};
-  if (type == PALQ_F32) cache_append_kernel<F32><<<g, 256, 0, s>>>(c, b, x);
-  else if (type == PALQ_F16) cache_append_kernel<F16><<<g, 256, 0, s>>>(c, b, x);
-  else cache_append_kernel<BF16><<<g, 256, 0, s>>>(c, b, x);
+  if (type == PALQ_F32) launch_append_t<F32>(g, c, b, x, s);
+  else if (type == PALQ_F16) launch_append_t<F16>(g, c, b, x, s);
+  else launch_append_t<BF16>(g, c, b, x, s);
   return hipGetLastError();
 }
 
