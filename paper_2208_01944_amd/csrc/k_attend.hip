@@ -784,10 +784,11 @@ bool attend_plan(AttendArgs &a, int cus) {
   a.block = block_rows(a, cus);
   const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
   const int64_t base = std::max<int64_t>(1, rt * a.c.heads * a.b.requests);
-  // Parts of a request's tokens, each at least a tile for every wave: until two
-  // workgroups stand on every CU (one of 32 rows: its waves hold twice the
-  // accumulators; 4 requests, 5 tokens, window 8191: 23 us in 8 parts, 26 in 16).
-  const int64_t most = std::max<int64_t>(1, (a.b.max_len + 255) / 256), want = (a.block == 32 ? 1 : 2) * cus;
+  // Parts of a request's tokens, until two workgroups stand on every CU (one of 32
+  // rows: its waves hold twice the accumulators; 4 requests, 5 tokens, window 8191: 23 us
+  // in 8 parts, 26 in 16).  A part has two tiles or more for every wave, and what is
+  // done in four is not cut at all: joining costs as much.
+  const int64_t most = a.b.max_len <= 1024 ? 1 : (a.b.max_len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), want / base));
   return base * a.splits < (int64_t)1 << 31;
 }

@@ -156,12 +156,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   const int c0 = grown ? 0 : kept >> 4, pieces = ((end + 15) >> 4) - c0;
   for (int p = threadIdx.x; p < pieces * D; p += 256) {
     const int d = p / pieces, at = (c0 + p % pieces) * 16;
-    v4i *piece = (v4i *)(dst + d * c.page + at);
-    v4i o = {0, 0, 0, 0};
-    if (at < kept) {
-      o = *piece;
-      if (grown) o = rescale16(o, ratio);
+    int8_t *to = dst + d * c.page;
+    if (at < kept && !grown) {  // only what is new: the old codes need not come first
+      for (int t = kept; t < min(end, at + 16); ++t) to[t] = (int8_t)(turned[d * words + (t >> 2)] >> (8 * (t & 3)));
+      continue;
     }
+    v4i *piece = (v4i *)(to + at);
+    v4i o = {0, 0, 0, 0};
+    if (at < kept) o = rescale16(*piece, ratio);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int t = at + 4 * j;

@@ -280,8 +280,6 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_one_kernel(LinearArg
 // both operands' slabs are copied from memory straight into LDS (two stages, one
 // in use, one on its way), and a wave reads the operands of the next 32 k while
 // the matrix cores work on the present ones, across the stage's barrier too.
-constexpr int kStageK = 128;
-
 // 16 bytes per lane from the buffer into LDS at `dst` (uniform) + 16 lane; in asm,
 // so that the compiler does not order LDS reads after them: the stages' waits and
 // barriers do.
@@ -302,19 +300,19 @@ __device__ __forceinline__ void stage_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
-template <int WC, int WT, int CT, int TT, int S>
+template <int WC, int WT, int CT, int TT, int S, int KB>
 struct TileShape {
   static constexpr int C = 32 * CT * WC, M = 32 * TT * WT, WAVES = WC * WT;
-  static constexpr int STAGE = (C + M) * kStageK;                   // bytes of one stage
+  static constexpr int STAGE = (C + M) * 64 * KB;                   // bytes of one stage
   static constexpr int OUT = 32 * (32 * CT + 4) * 4 * WAVES;        // the epilogue's: 32 tokens of every wave
   static constexpr int LDS = S * STAGE > OUT ? S * STAGE : OUT;
-  static constexpr int LOADS = (C + M) / 16 * 2 / WAVES;            // 1 KB loads of a wave for a stage
-  static_assert((C + M) / 16 * 2 % WAVES == 0, "");
+  static constexpr int LOADS = (C + M) / 16 * KB / WAVES;            // 1 KB loads of a wave for a stage
+  static_assert((C + M) / 16 * KB % WAVES == 0, "");
 };
 
-template <class T, int WC, int WT, int CT, int TT, int S>
+template <class T, int WC, int WT, int CT, int TT, int S, int KB>
 __global__ __launch_bounds__(64 * WC * WT, 2) void linear_tile_kernel(LinearArgs a, int ctiles, int mtiles, int band) {
-  typedef TileShape<WC, WT, CT, TT, S> G;
+  typedef TileShape<WC, WT, CT, TT, S, KB> G;
   typedef typename T::raw R;
   __shared__ __attribute__((aligned(1024))) uint8_t lds[G::LDS];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -329,31 +327,28 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void linear_tile_kernel(LinearArgs
   const int b0 = t / (band * ctiles) * band, inb = min(band, mtiles - b0), rem = t - b0 * ctiles;
   const int ct0 = rem / inb, mt0 = b0 + rem % inb;
 
-  const int kb = a.kp / 64, stages = a.kp / kStageK;
+  const int kb = a.kp / 64, stages = kb / KB;
   const v4i rw = buffer_of(a.w + (int64_t)ct0 * (G::C / 16) * kb * 1024);
   const v4i rx = buffer_of(a.x + (int64_t)mt0 * (G::M / 16) * kb * 1024);
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)lds;
-  // a stage in LDS: 16-row slabs of the channels, then of the tokens, two slabs (128 k) each
-  auto fetch = [&](int s, int slot) __attribute__((always_inline)) {
-    const uint32_t at = base + (uint32_t)slot * G::STAGE;
-#pragma unroll
-    for (int i = 0; i < G::LOADS; ++i) {
-      const int piece = i * G::WAVES + wave, slab = piece >> 1;  // uniform
-      const bool w = slab < G::C / 16;
-      const uint32_t soff = (uint32_t)(((w ? slab : slab - G::C / 16) * kb + 2 * s + (piece & 1)) * 1024);
-      to_lds(w ? rw : rx, at + piece * 1024, lane * 16, soff);
-    }
+  // a stage in LDS: 16-row slabs of the channels, then of the tokens, KB slabs (64 k each) a row of them
+  auto fetch = [&](int s, int slot, int i) __attribute__((always_inline)) {
+    const int piece = i * G::WAVES + wave, slab = piece / KB;  // uniform
+    const bool w = slab < G::C / 16;
+    const uint32_t soff = (uint32_t)(((w ? slab : slab - G::C / 16) * kb + KB * s + piece % KB) * 1024);
+    to_lds(w ? rw : rx, base + (uint32_t)slot * G::STAGE + piece * 1024, lane * 16, soff);
   };
   // operands of 32 k: lane l has row l % 32, 16 k from l / 32
   struct Ops { v4i w[CT], x[TT]; };
-  const int lo = (lane & 15) * 16 + (lane >> 4 & 1) * 2048 + (lane >> 5) * 256;
-  const int wo = lo + wc * CT * 4096, xo = lo + G::C * kStageK + wt * TT * 4096;
+  constexpr int R32 = 2048 * KB;  // LDS bytes of 32 rows
+  const int lo = (lane & 15) * 16 + (lane >> 4 & 1) * 1024 * KB + (lane >> 5) * 256;
+  const int wo = lo + wc * CT * R32, xo = lo + G::C * 64 * KB + wt * TT * R32;
   auto read = [&](Ops &o, int slot, int step) __attribute__((always_inline)) {
     const uint8_t *p = lds + slot * G::STAGE + (step >> 1) * 1024 + (step & 1) * 512;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) o.w[c] = *(const v4i *)(p + wo + c * 4096);
+    for (int c = 0; c < CT; ++c) o.w[c] = *(const v4i *)(p + wo + c * R32);
 #pragma unroll
-    for (int m = 0; m < TT; ++m) o.x[m] = *(const v4i *)(p + xo + m * 4096);
+    for (int m = 0; m < TT; ++m) o.x[m] = *(const v4i *)(p + xo + m * R32);
   };
   v16i acc[CT][TT];
 #pragma unroll
@@ -362,39 +357,48 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void linear_tile_kernel(LinearArgs
     for (int m = 0; m < TT; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[c][m][i] = 0;
-  auto multiply = [&](const Ops &o) __attribute__((always_inline)) {
-#pragma unroll
-    for (int m = 0; m < TT; ++m)
-#pragma unroll
-      for (int c = 0; c < CT; ++c) acc[c][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.w[c], o.x[m], acc[c][m], 0, 0, 0);
-  };
-
-  // S stages: one in use, the next S - 1 in LDS or on their way
+  // S stages: one in use, the next S - 1 in LDS or on their way.  A stage is asked for
+  // load by load between the products of the stage S before it: asked for at once, its
+  // loads keep the wave from issuing products.
+  constexpr int STEPS = 2 * KB;
   Ops ops[2];
 #pragma unroll
   for (int s = 0; s < S; ++s)
-    if (s < stages) fetch(s, s);
+    if (s < stages)
+#pragma unroll
+      for (int i = 0; i < G::LOADS; ++i) fetch(s, s, i);
   if (stages >= S) stage_barrier<G::LOADS * (S - 1)>();
   else stage_barrier<0>();
   read(ops[0], 0, 0);
-  int slot = 0;
+  int slot = 0, last = S - 1;  // places of stages s and s - 1
   for (int s = 0; s < stages; ++s) {
     const int next = slot + 1 == S ? 0 : slot + 1;
-    read(ops[1], slot, 1);
-    multiply(ops[0]);
-    read(ops[0], slot, 2);
-    multiply(ops[1]);
-    read(ops[1], slot, 3);
-    multiply(ops[0]);
-    // every read of stage s is done and stage s + 1 has landed (the S - 2 after it may
-    // be on their way); the place of s takes stage s + S
-    if (s + S <= stages) stage_barrier<G::LOADS * (S - 2)>();
-    else stage_barrier<0>();
-    if (s + 1 < stages) {
-      if (s + S < stages) fetch(s + S, slot);
-      read(ops[0], next, 0);
+    const bool more = s > 0 && s - 1 + S < stages;  // (the place of s - 1 is free since the last barrier)
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+      if (j == STEPS - 1) {
+        // every read of stage s is done and stage s + 1 has landed (those after it may
+        // be on their way)
+        if (s + S <= stages) stage_barrier<G::LOADS * (S - 2)>();
+        else stage_barrier<0>();
+        if (s + 1 < stages) read(ops[0], next, 0);
+      } else {
+        read(ops[(j + 1) & 1], slot, j + 1);
+      }
+      const Ops &o = ops[j & 1];
+#pragma unroll
+      for (int m = 0; m < TT; ++m)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          acc[c][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(o.w[c], o.x[m], acc[c][m], 0, 0, 0);
+          constexpr int N = CT * TT * (STEPS - 1);           // products before the last step
+          const int n = (j * TT + m) * CT + c;
+          if (j < STEPS - 1 && n * G::LOADS / N != (n + 1) * G::LOADS / N && more)
+#pragma unroll
+            for (int i = n * G::LOADS / N; i < (n + 1) * G::LOADS / N; ++i) fetch(s - 1 + S, last, i);
+        }
     }
-    multiply(ops[1]);
+    last = slot;
     slot = next;
   }
 
@@ -454,11 +458,11 @@ __global__ __launch_bounds__(64 * WC * WT, 2) void linear_tile_kernel(LinearArgs
   }
 }
 
-template <class T, int WC, int WT, int CT, int TT, int S>
+template <class T, int WC, int WT, int CT, int TT, int S, int KB>
 void launch_tile(const LinearArgs &a, hipStream_t s) {
-  typedef TileShape<WC, WT, CT, TT, S> G;
+  typedef TileShape<WC, WT, CT, TT, S, KB> G;
   const int ctiles = (a.n_out + G::C - 1) / G::C, mtiles = (int)((a.rows + G::M - 1) / G::M), per = (ctiles * mtiles + 7) / 8;
-  linear_tile_kernel<T, WC, WT, CT, TT, S><<<(unsigned)(per * 8), 64 * WC * WT, 0, s>>>(a, ctiles, mtiles, 4);
+  linear_tile_kernel<T, WC, WT, CT, TT, S, KB><<<(unsigned)(per * 8), 64 * WC * WT, 0, s>>>(a, ctiles, mtiles, 4);
 }
 template <class T, int MT, int NT>
 void launch_few(const LinearArgs &a, hipStream_t s) {
@@ -469,14 +473,16 @@ void launch_few(const LinearArgs &a, hipStream_t s) {
 template <class T>
 hipError_t launch_linear_t(const LinearArgs &a, hipStream_t s) {
   // The largest tile that still gives (nearly) every CU one: operands are then read
-  // least often.  Measured with the quantiser, 4096 x 4096 weights: 64 rows 9.7 us on
-  // linear_few, 14.6 on 64 x 64 tiles; 512 rows 22.9 on 64 x 64, 29.5 on 128 x 128;
-  // 2048 rows 49 on 128 x 128, 60 on 256 x 256; 8192 x 8192, 4096 rows: 267 on 256 x 256,
-  // 298 on 128 x 128.
+  // least often.  Measured with the quantiser, bf16, 4096 x 4096 weights: 64 rows 9.7 us
+  // on linear_few, 14.6 on 64 x 64 tiles; 512 rows 22.3 on 64 x 64, 25.0 on 128 x 128;
+  // 1024 rows (a 128 x 128 tile a CU) 29.3 with 8 waves and 4 stages of 128 k, 32.6 with 4
+  // waves and 3 of 64, which lets three stand on a CU: 2048 rows 50 and 55; 4096 rows 79 on
+  // 256 x 256, 94 on 128 x 128.
   auto tiles = [&](int t) { return ((a.n_out + t - 1) / t) * ((a.rows + t - 1) / t); };
-  if (tiles(256) >= 192) launch_tile<T, 2, 4, 4, 2, 2>(a, s);
-  else if (tiles(128) >= 256) launch_tile<T, 2, 2, 2, 2, 2>(a, s);
-  else if (a.rows > 32 && tiles(64) >= 256) launch_tile<T, 2, 2, 1, 1, 4>(a, s);
+  if (tiles(256) >= 192) launch_tile<T, 4, 2, 2, 4, 4, 1>(a, s);
+  else if (tiles(128) >= 512) launch_tile<T, 2, 2, 2, 2, 3, 1>(a, s);
+  else if (tiles(128) >= 256) launch_tile<T, 2, 4, 2, 1, 4, 2>(a, s);
+  else if (a.rows > 32 && tiles(64) >= 256) launch_tile<T, 2, 2, 1, 1, 4, 2>(a, s);
   else if (a.rows > 16) launch_few<T, 2, 2>(a, s);
   else launch_few<T, 1, 1>(a, s);
   return hipGetLastError();
