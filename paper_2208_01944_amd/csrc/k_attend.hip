@@ -74,11 +74,6 @@ __device__ __forceinline__ RowScale row_scale(uint32_t mag) {
   return {e == 255 ? 0.0f : __uint_as_float((uint32_t)(254 - b) << 23), __uint_as_float((uint32_t)b << 23)};
 }
 
-// 8 consecutive elements at p, which is aligned to elements only, two in a word.
-__device__ __forceinline__ void load_words(const uint16_t *p, v4i &raw) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) raw[i] = (int)((uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16);
-}
 template <class T>
 __device__ __forceinline__ float low(int w) { return T::get((uint16_t)((uint32_t)w & 0xffffu)); }
 template <class T>
@@ -130,7 +125,6 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   // the rows' elements are on their way while the tokens' pages are looked up
   v4i raw[NQ][KS];
   int rlo[NQ], rhi[NQ];
-  const bool vec = (((uintptr_t)a.q | (uintptr_t)(a.q_row * 2) | (uintptr_t)(a.q_head * 2)) & 15u) == 0;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int row = first + n * 16 + col;
@@ -142,13 +136,8 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     // this lane's channels of row lane % 16 (of the first row past the last): of every
     // 64 (32 where 64 do not divide the head) the 16 (8) from 16 c (8 c) on, as the keys'
     const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * CH;
-    if (vec) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) raw[n][s] = *(const v4i *)(p + s * 8 / CH * 4 * CH + s * 8 % CH);
-    } else {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) load_words(p + s * 8 / CH * 4 * CH + s * 8 % CH, raw[n][s]);
-    }
+    for (int s = 0; s < KS; ++s) raw[n][s] = load_any(p + s * 8 / CH * 4 * CH + s * 8 % CH);
   }
   v4f O[NQ][DT];
   float M[NQ], L[NQ];
@@ -338,7 +327,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
         uint16_t *dst = a.out + (q.row0 + t) * a.out_row + (int64_t)hq * a.out_head + d;
-        store4<T>(dst, v, (((uintptr_t)a.out | (uintptr_t)(a.out_row * 2) | (uintptr_t)(a.out_head * 2)) & 7u) == 0);
+        store4<T>(dst, v);
       } else {
         const int64_t hs = (int64_t)cv.heads * a.group;
         const int64_t at = ((int64_t)split * a.b.tokens + q.row0 + t) * hs + hq;
@@ -430,16 +419,10 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   h8 Q[KS];
   float f;
   {
-    const bool vec = (((uintptr_t)a.q | (uintptr_t)(a.q_row * 2) | (uintptr_t)(a.q_head * 2)) & 15u) == 0;
-    const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)hq * a.q_head + c * 8;
+      const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)hq * a.q_head + c * 8;
     v4i raw[KS];
-    if (vec) {
 #pragma unroll
-      for (int s = 0; s < KS; ++s) raw[s] = *(const v4i *)(p + s * 16);
-    } else {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) load_words(p + s * 16, raw[s]);
-    }
+    for (int s = 0; s < KS; ++s) raw[s] = load_any(p + s * 16);
     uint32_t mag = largest<T, KS>(raw);
     mag = max(mag, (uint32_t)__shfl_xor((int)mag, 32));
     RowScale rs = row_scale(mag);
@@ -678,23 +661,17 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const float v[4] = {O[d][4 * g] * inv, O[d][4 * g + 1] * inv, O[d][4 * g + 2] * inv, O[d][4 * g + 3] * inv};
-      store4<T>(my + col * LD + d * 32 + g * 8 + c * 4, v, true);
+      store4<T>(my + col * LD + d * 32 + g * 8 + c * 4, v);
     }
   __builtin_amdgcn_wave_barrier();
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  const bool vec = (((uintptr_t)a.out | (uintptr_t)(a.out_row * 2) | (uintptr_t)(a.out_head * 2)) & 15u) == 0;
   for (int p = lane; p < 32 * (D / 8); p += 64) {
     const int rr = p / (D / 8), e = p % (D / 8) * 8, orow = first + wave * 32 + rr;
     if (orow >= rows) continue;
     const int ot = orow / a.group, oh = h * a.group + orow - ot * a.group;
     const v4i o = *(const v4i *)(my + rr * LD + e);
     uint16_t *dst = a.out + (q.row0 + ot) * a.out_row + (int64_t)oh * a.out_head + e;
-    if (vec) {
-      *(v4i *)dst = o;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) dst[i] = (uint16_t)((uint32_t)o[i >> 1] >> (16 * (i & 1)));
-    }
+    store_any(dst, o);
   }
 }
 
@@ -738,7 +715,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   uint16_t *dst = a.out + (q.row0 + t) * a.out_row + hq * a.out_head + d;
-  store4<T>(dst, v, (((uintptr_t)a.out | (uintptr_t)(a.out_row * 2) | (uintptr_t)(a.out_head * 2)) & 7u) == 0);
+  store4<T>(dst, v);
 }
 
 // Rows of a workgroup: 16 or 32 on attend_rows_kernel, 128 on attend_tile_kernel.

@@ -68,7 +68,6 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   const R *src = (const R *)(values ? x.v : x.k);
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
   src += (q.row0 + (t0 - (q.len - q.n))) * row + h * head;  // row of token t0 (there may be none)
-  const bool vec = (((uintptr_t)(values ? x.v : x.k) | (uintptr_t)(row * (int64_t)sizeof(R)) | (uintptr_t)(head * (int64_t)sizeof(R))) & 15u) == 0;
   const int64_t ph = (int64_t)pid * c.heads + h;
   float *scale = (values ? c.vs : c.ks) + ph;
   const float had = kept ? *scale : 0.0f;
@@ -82,25 +81,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
     for (int t = 0; t < 4; ++t) {
       const bool here = p < items && tq + t >= kept && tq + t < end;
       const R *from = src + (int64_t)(tq + t) * row + ch;
-      if (here && vec) {
-        if constexpr (sizeof(R) == 4) {
-          const v4f a = ((const v4f *)from)[0], e = ((const v4f *)from)[1];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            v[i][t][j] = a[j];
-            v[i][t][4 + j] = e[j];
-          }
-        } else {
-          const v4i a = *(const v4i *)from;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            v[i][t][2 * j] = T::get((uint16_t)((uint32_t)a[j] & 0xffffu));
-            v[i][t][2 * j + 1] = T::get((uint16_t)((uint32_t)a[j] >> 16));
-          }
-        }
+      if (here) {
+        load8<T>(from, v[i][t]);
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][t][j] = here ? T::get(from[j]) : 0.0f;
+        for (int j = 0; j < 8; ++j) v[i][t][j] = 0.0f;
       }
     }
 #pragma unroll
@@ -196,7 +181,6 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
   const int8_t *src = (values ? c.v : c.k) + ph * c.page * D;
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
   R *dst = (R *)(values ? x.v : x.k) + (q.row0 + (lo - (q.len - q.n))) * row + h * head;
-  const bool al = (((uintptr_t)dst | (uintptr_t)(row * sizeof(R))) & (4 * sizeof(R) - 1)) == 0;
   // several pieces' loads in flight before the first store
   if (!values) {
     const int quads = D / 4, all = (hi - lo) * quads;
@@ -212,7 +196,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
         float v[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = (float)(int8_t)(w[i] >> (8 * j)) * s;
-        store4<T>(dst + (int64_t)t * row + d, v, al);
+        store4<T>(dst + (int64_t)t * row + d, v);
       }
     }
   } else {

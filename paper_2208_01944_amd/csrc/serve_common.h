@@ -47,48 +47,61 @@ struct BF16 { typedef uint16_t raw;
               static __device__ __forceinline__ float get(raw v) { return __uint_as_float((uint32_t)v << 16); }
               static __device__ __forceinline__ raw put(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); } };
 
-// Four consecutive values to p (aligned: p allows one store).
+// 16 and 8 bytes at any address: the hardware's vector loads and stores need no
+// alignment, and odd row lengths must not cost a load for every element.
+__device__ __forceinline__ v4i load_any(const void *p) {
+  v4i v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+template <class V>
+__device__ __forceinline__ void store_any(void *p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
+
+// Four consecutive values to p.
 template <class T>
-__device__ __forceinline__ void store4(typename T::raw *p, const float *v, bool aligned) {
-  if (aligned) {
-    if constexpr (sizeof(typename T::raw) == 4) {
-      *(v4f *)p = v4f{v[0], v[1], v[2], v[3]};
-    } else {
-      const uint32_t a = (uint32_t)T::put(v[0]) | (uint32_t)T::put(v[1]) << 16;
-      const uint32_t b = (uint32_t)T::put(v[2]) | (uint32_t)T::put(v[3]) << 16;
-      *(v2i *)p = v2i{(int)a, (int)b};
-    }
+__device__ __forceinline__ void store4(typename T::raw *p, const float *v) {
+  if constexpr (sizeof(typename T::raw) == 4) {
+    store_any(p, v4f{v[0], v[1], v[2], v[3]});
   } else {
-    for (int i = 0; i < 4; ++i) p[i] = T::put(v[i]);
+    const uint32_t a = (uint32_t)T::put(v[0]) | (uint32_t)T::put(v[1]) << 16;
+    const uint32_t b = (uint32_t)T::put(v[2]) | (uint32_t)T::put(v[3]) << 16;
+    store_any(p, v2i{(int)a, (int)b});
   }
 }
 
-// Sixteen consecutive values from p, of which the first n exist (the others
-// are 0); vec: p is 16-byte aligned.
+// Eight consecutive values from p.
 template <class T>
-__device__ __forceinline__ void load16(const typename T::raw *p, int n, bool vec, float *v) {
-  if (vec && n >= 16) {
-    if constexpr (sizeof(typename T::raw) == 4) {
+__device__ __forceinline__ void load8(const typename T::raw *p, float *v) {
+  const v4i a = load_any(p);
+  if constexpr (sizeof(typename T::raw) == 4) {
+    const v4i b = load_any(p + 4);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const v4f x = ((const v4f *)p)[q];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * q + i] = x[i];
-      }
-    } else {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const v4i x = ((const v4i *)p)[q];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[8 * q + 2 * i] = T::get((uint16_t)((uint32_t)x[i] & 0xffffu));
-          v[8 * q + 2 * i + 1] = T::get((uint16_t)((uint32_t)x[i] >> 16));
-        }
-      }
+    for (int i = 0; i < 4; ++i) {
+      v[i] = __int_as_float(a[i]);
+      v[4 + i] = __int_as_float(b[i]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = i < n ? T::get(p[i]) : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = T::get((uint16_t)((uint32_t)a[i] & 0xffffu));
+      v[2 * i + 1] = T::get((uint16_t)((uint32_t)a[i] >> 16));
+    }
+  }
+}
+
+// Sixteen consecutive values from p, of which the first n exist (the others are
+// 0; n may be 0 or less, and p[n - 1] is there in any case).
+template <class T>
+__device__ __forceinline__ void load16(const typename T::raw *p, int n, float *v) {
+  if (n >= 16) {
+    load8<T>(p, v);
+    load8<T>(p + 8, v + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {  // (every load in flight: none waits for a condition)
+      const float x = T::get(p[min(i, n - 1)]);
+      v[i] = i < n ? x : 0.0f;
+    }
   }
 }
 
