@@ -484,8 +484,8 @@ palq_status palq_linear_run(palq_ctx *ctx, const palq_linear *lin, const void *x
                             const float *x_scale, int64_t rows, void *y, int32_t y_type, int64_t y_ld);
 /* Frees a layer (waits for device work that still reads it). */
 void palq_linear_destroy(palq_linear *lin);
-/* The kernel a run of `rows` rows takes (static host string; "" for a
- * validate-only layer, NULL for a null one). */
+/* The kernel a run of `rows` floating rows takes (static host string; "" for
+ * a validate-only layer, NULL for a null one). */
 const char *palq_linear_kernels(const palq_linear *lin, int64_t rows);
 
 /* A paged key/value cache of one layer.  A page holds page_tokens (16, 32, 64

@@ -195,22 +195,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArg
   }
 }
 
-// A token or a few of floating values: every workgroup quantises the rows by itself,
-// into LDS, while its first weights are on their way; one launch instead of two.
-// It goes through its 16-channel tiles with the same rows.
-struct RawRows { const void *x; int64_t ld; int32_t n_in; };
-constexpr int kOneRows = 8, kOneBytes = 64 << 10;  // at most: rows, and bytes of their codes
+// One token of floating values: every workgroup quantises the row by itself, into
+// LDS, while its first weights are on their way; one launch instead of two.  It goes
+// through its 16-channel tiles with the same row.  At most 128 registers, so that two
+// workgroups on a CU keep twice the weights in flight.  4096 x 4096 weights 4.9 us (7.2
+// with the quantiser apart), 8192 x 8192 12.1 us, 5.5 TB/s.  (Three rows this way need
+// 156 registers: 8192 x 8192 17.8 us, against 15.6 in two launches.)
+struct RawRow { const void *x; int32_t n_in; };
+constexpr int kOneBytes = 16 << 10;  // at most: bytes of the row's codes
 
 template <class T, class X>
-__global__ __launch_bounds__(64 * kFewWaves, 2) void linear_one_kernel(LinearArgs a, RawRows r) {
-  extern __shared__ __attribute__((aligned(16))) uint8_t codes[];  // [rows][kp]
+__global__ __launch_bounds__(64 * kFewWaves, 4) void linear_one_kernel(LinearArgs a, RawRow r) {
+  __shared__ __attribute__((aligned(16))) uint8_t codes[kOneBytes];
   constexpr int TH = 64 * kFewWaves, U = 8;
   __shared__ v4i part[kFewWaves][64];
-  __shared__ uint32_t mags[kOneRows][kFewWaves];
-  __shared__ float scales[kOneRows];
-  typedef typename X::raw R;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, kb = a.kp / 64, rows = (int)a.rows;
-  const int tiles = (a.n_out + 15) / 16;
+  __shared__ uint32_t mags[kFewWaves];
+  const typename X::raw *x = (const typename X::raw *)r.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, kb = a.kp / 64, tiles = (a.n_out + 15) / 16;
   v4i wv[U];
   auto fetch = [&](int tile, int k) __attribute__((always_inline)) {
     const v4i *w = (const v4i *)(a.w + (int64_t)min(tile, tiles - 1) * kb * 1024) + lane;
@@ -218,34 +219,35 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_one_kernel(LinearArg
     for (int u = 0; u < U; ++u) wv[u] = w[(int64_t)min(k + u * kFewWaves, kb - 1) * 64];
   };
   fetch(blockIdx.x, wave);
-  // largest magnitudes, then codes: pieces of 16 columns, a thread every TH-th
-  const int pieces = a.kp / 16;
-  for (int i = 0; i < rows; ++i) {
-    uint32_t mag = 0;
-    for (int p = threadIdx.x; p < pieces; p += TH) {
-      float v[16];
-      load16<X>((const R *)r.x + i * r.ld + p * 16, r.n_in - p * 16, v);
+  // largest magnitude, then codes: pieces of 16 columns, a thread every TH-th, its first
+  // held between the two
+  const int pieces = a.kp / 16, own = threadIdx.x;
+  float held[16];
+  load16<X>(x + min(own, pieces - 1) * 16, r.n_in - min(own, pieces - 1) * 16, held);
+  uint32_t mag = 0;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) mag = max(mag, mag_bits(v[j]));
-    }
-    mag = wave_max(mag);
-    if (lane == 0) mags[i][wave] = mag;
+  for (int j = 0; j < 16; ++j) mag = max(mag, mag_bits(held[j]));
+  for (int p = own + TH; p < pieces; p += TH) {
+    float v[16];
+    load16<X>(x + p * 16, r.n_in - p * 16, v);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) mag = max(mag, mag_bits(v[j]));
+  }
+  mag = wave_max(mag);
+  if (lane == 0) mags[wave] = mag;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) mag = max(mag, mags[w]);
+  const float s = scale_of(mag), inv = inverse_of(s);
+  const v4i zero = {0, 0, 0, 0};
+  if (own < pieces) *(v4i *)(codes + own * 16) = s == s ? quantize16(held, inv) : zero;
+  for (int p = own + TH; p < pieces; p += TH) {
+    float v[16];
+    load16<X>(x + p * 16, r.n_in - p * 16, v);
+    *(v4i *)(codes + p * 16) = s == s ? quantize16(v, inv) : zero;
   }
   __syncthreads();
-  for (int i = 0; i < rows; ++i) {
-    uint32_t mag = mags[i][0];
-#pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) mag = max(mag, mags[i][w]);
-    const float s = scale_of(mag), inv = inverse_of(s);
-    if (threadIdx.x == 0) scales[i] = s;
-    for (int p = threadIdx.x; p < pieces; p += TH) {
-      float v[16];
-      load16<X>((const R *)r.x + i * r.ld + p * 16, r.n_in - p * 16, v);
-      *(v4i *)(codes + (int64_t)i * a.kp + p * 16) = s == s ? quantize16(v, inv) : v4i{0, 0, 0, 0};
-    }
-  }
-  __syncthreads();
-  const uint8_t *mine = codes + (int64_t)min(lane & 15, rows - 1) * a.kp + (lane >> 4) * 16;
+  const uint8_t *mine = codes + (lane >> 4) * 16;  // (all 16 columns of the product are this row)
   for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
     v4i acc = {0, 0, 0, 0};
     for (int k = wave; k < kb; k += kFewWaves * U) {
@@ -259,10 +261,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_one_kernel(LinearArg
     part[wave][lane] = acc;
     __syncthreads();
     if (wave == 0) {
-      v4i s = part[0][lane];
+      v4i sum = part[0][lane];
 #pragma unroll
-      for (int w = 1; w < kFewWaves; ++w) s += part[w][lane];
-      put_quad<T>(a, lane & 15, tile * 16 + (lane >> 4) * 4, s, scales[min(lane & 15, rows - 1)]);
+      for (int w = 1; w < kFewWaves; ++w) sum += part[w][lane];
+      put_quad<T>(a, lane & 15, tile * 16 + (lane >> 4) * 4, sum, s);
     }
     __syncthreads();
   }
@@ -463,31 +465,42 @@ void launch_few(const LinearArgs &a, hipStream_t s) {
                                  64 * kFewWaves, 0, s>>>(a);
 }
 
+// The kernel for this many rows and channels.  The largest tile that still gives
+// (nearly) every CU one: operands are then read least often.  Measured with the
+// quantiser, bf16, 4096 x 4096 weights: 64 rows 9.7 us on linear_few, 14.6 on 64 x 64
+// tiles; 512 rows 22.3 on 64 x 64, 25.0 on 128 x 128; 1024 rows (a 128 x 128 tile a CU) 29.3
+// with 8 waves and 4 stages of 128 k, 32.6 with 4 waves and 3 of 64, which lets three stand
+// on a CU: 2048 rows 50 and 55; 4096 rows 79 on 256 x 256, 94 on 128 x 128.
+enum LinearKind { kFew1, kFew2, kTile64, kTile128, kTile128Many, kTile256 };
+LinearKind linear_kind(int64_t rows, int n_out) {
+  auto tiles = [&](int t) { return ((n_out + t - 1) / t) * ((rows + t - 1) / t); };
+  if (tiles(256) >= 192) return kTile256;
+  if (tiles(128) >= 512) return kTile128Many;
+  if (tiles(128) >= 256) return kTile128;
+  if (rows > 32 && tiles(64) >= 256) return kTile64;
+  return rows > 16 ? kFew2 : kFew1;
+}
+
 template <class T>
 hipError_t launch_linear_t(const LinearArgs &a, hipStream_t s) {
-  // The largest tile that still gives (nearly) every CU one: operands are then read
-  // least often.  Measured with the quantiser, bf16, 4096 x 4096 weights: 64 rows 9.7 us
-  // on linear_few, 14.6 on 64 x 64 tiles; 512 rows 22.3 on 64 x 64, 25.0 on 128 x 128;
-  // 1024 rows (a 128 x 128 tile a CU) 29.3 with 8 waves and 4 stages of 128 k, 32.6 with 4
-  // waves and 3 of 64, which lets three stand on a CU: 2048 rows 50 and 55; 4096 rows 79 on
-  // 256 x 256, 94 on 128 x 128.
-  auto tiles = [&](int t) { return ((a.n_out + t - 1) / t) * ((a.rows + t - 1) / t); };
-  if (tiles(256) >= 192) launch_tile<T, 4, 2, 2, 4, 4, 1>(a, s);
-  else if (tiles(128) >= 512) launch_tile<T, 2, 2, 2, 2, 3, 1>(a, s);
-  else if (tiles(128) >= 256) launch_tile<T, 2, 4, 2, 1, 4, 2>(a, s);
-  else if (a.rows > 32 && tiles(64) >= 256) launch_tile<T, 2, 2, 1, 1, 4, 2>(a, s);
-  else if (a.rows > 16) launch_few<T, 2, 2>(a, s);
-  else launch_few<T, 1, 1>(a, s);
+  switch (linear_kind(a.rows, a.n_out)) {
+    case kFew1: launch_few<T, 1, 1>(a, s); break;
+    case kFew2: launch_few<T, 2, 2>(a, s); break;
+    case kTile64: launch_tile<T, 2, 2, 1, 1, 4, 2>(a, s); break;
+    case kTile128: launch_tile<T, 2, 4, 2, 1, 4, 2>(a, s); break;
+    case kTile128Many: launch_tile<T, 2, 2, 2, 2, 3, 1>(a, s); break;
+    case kTile256: launch_tile<T, 4, 2, 2, 4, 4, 1>(a, s); break;
+  }
   return hipGetLastError();
 }
 
 template <class T, class X>
-void launch_one_t(const LinearArgs &a, const RawRows &r, hipStream_t s) {
+void launch_one_t(const LinearArgs &a, const RawRow &r, hipStream_t s) {
   const unsigned tiles = (unsigned)((a.n_out + 15) / 16);
-  linear_one_kernel<T, X><<<std::min(tiles, 512u), 64 * kFewWaves, (size_t)a.rows * a.kp, s>>>(a, r);
+  linear_one_kernel<T, X><<<std::min(tiles, 512u), 64 * kFewWaves, 0, s>>>(a, r);
 }
 template <class T>
-void launch_one_x(const LinearArgs &a, const RawRows &r, int x_type, hipStream_t s) {
+void launch_one_x(const LinearArgs &a, const RawRow &r, int x_type, hipStream_t s) {
   if (x_type == PALQ_F32) launch_one_t<T, F32>(a, r, s);
   else if (x_type == PALQ_F16) launch_one_t<T, F16>(a, r, s);
   else launch_one_t<T, BF16>(a, r, s);
@@ -531,16 +544,19 @@ hipError_t launch_linear(const LinearArgs &a, int y_type, hipStream_t s) {
   return launch_linear_t<BF16>(a, s);
 }
 
-bool linear_one(int64_t rows, int32_t kp) { return rows <= kOneRows && rows * kp <= kOneBytes; }
+bool linear_one(int64_t rows, int32_t kp) { return rows == 1 && kp <= kOneBytes; }
 
-hipError_t launch_linear_one(const LinearArgs &a, const void *x, int x_type, int64_t x_ld, int32_t n_in, int y_type, hipStream_t s) {
-  const RawRows r{x, x_ld, n_in};
+hipError_t launch_linear_one(const LinearArgs &a, const void *x, int x_type, int32_t n_in, int y_type, hipStream_t s) {
+  const RawRow r{x, n_in};
   if (y_type == PALQ_F32) launch_one_x<F32>(a, r, x_type, s);
   else if (y_type == PALQ_F16) launch_one_x<F16>(a, r, x_type, s);
   else launch_one_x<BF16>(a, r, x_type, s);
   return hipGetLastError();
 }
 
-const char *linear_kernel_label(int64_t rows, int n_in, int n_out) { return "linear_few_kernel"; }
+const char *linear_kernel_label(int64_t rows, int n_out, int kp) {
+  if (linear_one(rows, kp)) return "linear_one_kernel";
+  return linear_kind(rows, n_out) <= kFew2 ? "linear_few_kernel" : "linear_tile_kernel";
+}
 
 }  // namespace palq

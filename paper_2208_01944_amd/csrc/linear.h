@@ -25,9 +25,10 @@ hipError_t launch_quantize_rows(const void *x, int type, int64_t rows, int cols,
 hipError_t launch_slabs(const int8_t *x, int64_t rows, int64_t padded_rows, int cols, int64_t ld, int kp, int8_t *out,
                         hipStream_t s);
 hipError_t launch_linear(const LinearArgs &a, int y_type, hipStream_t s);
-// Whether a product of floating rows runs as one launch from them (no slabs of x).
+// Whether a product of floating rows (one row) runs as one launch from them, without slabs of x.
 bool linear_one(int64_t rows, int32_t kp);
-hipError_t launch_linear_one(const LinearArgs &a, const void *x, int x_type, int64_t x_ld, int32_t n_in, int y_type, hipStream_t s);
-const char *linear_kernel_label(int64_t rows, int n_in, int n_out);
+hipError_t launch_linear_one(const LinearArgs &a, const void *x, int x_type, int32_t n_in, int y_type, hipStream_t s);
+// Of floating rows (codes never run as linear_one).
+const char *linear_kernel_label(int64_t rows, int n_out, int kp);
 
 }  // namespace palq

@@ -226,7 +226,7 @@ palq_status palq_linear_run(palq_ctx *ctx, const palq_linear *lin, const void *x
                lin->n_out, lin->kp};
   hipError_t e;
   if (x_type != PALQ_I8 && linear_one(rows, lin->kp)) {
-    e = launch_linear_one(a, x, x_type, x_ld, lin->n_in, y_type, ctx->stream);
+    e = launch_linear_one(a, x, x_type, lin->n_in, y_type, ctx->stream);
     return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "linear");
   }
   if (x_type == PALQ_I8) {
@@ -251,7 +251,7 @@ void palq_linear_destroy(palq_linear *lin) {
 
 const char *palq_linear_kernels(const palq_linear *lin, int64_t rows) {
   if (!lin) return nullptr;
-  return lin->device < 0 ? "" : linear_kernel_label(rows, lin->n_in, lin->n_out);
+  return lin->device < 0 ? "" : linear_kernel_label(rows, lin->n_out, lin->kp);
 }
 
 palq_status palq_cache_append(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *k, int64_t k_row,

@@ -332,28 +332,25 @@ class Context:
 
     def cache_append(self, cache: Cache, k, v, batch: Batch):
         """palq_cache_append: k, v [tokens, heads, head_dim] into the pages of their requests."""
-        kt, kr, kh = _rows3(k, batch, cache)
-        vt, vr, vh = _rows3(v, batch, cache)
-        if kt != vt or k.shape != v.shape:
-            raise PalqError(ERR_ARG, "k and v differ in type or shape")
-        self._check(_cache_append(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, kt))
+        t, kr, kh, vr, vh = _pair3(k, v, batch, cache)
+        st = _cache_append(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, t)
+        if st:
+            self._check(st)
 
     def cache_read(self, cache: Cache, k, v, batch: Batch):
         """palq_cache_read: the values of each request's last tokens into k, v [tokens, heads, head_dim]."""
-        kt, kr, kh = _rows3(k, batch, cache)
-        vt, vr, vh = _rows3(v, batch, cache)
-        if kt != vt or k.shape != v.shape:
-            raise PalqError(ERR_ARG, "k and v differ in type or shape")
-        self._check(_cache_read(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, kt))
+        t, kr, kh, vr, vh = _pair3(k, v, batch, cache)
+        st = _cache_read(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, t)
+        if st:
+            self._check(st)
 
     def attention(self, cache: Cache, q, out, batch: Batch, scale, causal=True, window=0):
         """palq_attention: q, out [tokens, q_heads, head_dim]."""
-        qt, qr, qh = _rows3(q, batch, cache, cache.q_heads_ok)
-        ot, orow, oh = _rows3(out, batch, cache, cache.q_heads_ok)
-        if qt != ot or q.shape != out.shape:
-            raise PalqError(ERR_ARG, "q and out differ in type or shape")
-        self._check(_attention(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, qt,
-                               scale, causal, window))
+        t, qr, qh, orow, oh = _pair3(q, out, batch, cache, True)
+        st = _attention(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, t, scale, causal,
+                        window)
+        if st:
+            self._check(st)
 
 
 class Linear:
@@ -379,15 +376,17 @@ class Linear:
 
     def run(self, x, y, x_scale=None):
         """y [rows, n_out] from x [rows, n_in]: floating values, or int8 codes with x_scale fp32 [rows]."""
+        (rows, n_in), (y_rows, n_out) = x.shape, y.shape
+        if n_in != self.n_in or y_rows != rows or n_out != self.n_out:
+            raise PalqError(ERR_ARG, "x or y does not have the layer's shape")
         xt, x_ld = _rows2(x)
         yt, y_ld = _rows2(y)
-        rows = x.shape[0]
-        if x.shape[1] != self.n_in or y.shape[0] != rows or y.shape[1] != self.n_out:
-            raise PalqError(ERR_ARG, "x or y does not have the layer's shape")
         if x_scale is not None:
             _need(x_scale, torch.float32, rows, "x_scale")
             x_scale = x_scale.data_ptr()
-        self.ctx._check(_linear_run(self.ctx.h, self.h, x.data_ptr(), xt, x_ld, x_scale, rows, y.data_ptr(), yt, y_ld))
+        st = _linear_run(self.ctx.h, self.h, x.data_ptr(), xt, x_ld, x_scale, rows, y.data_ptr(), yt, y_ld)
+        if st:
+            self.ctx._check(st)
 
     def __del__(self):
         h = getattr(self, "h", None)
@@ -421,9 +420,6 @@ class Cache:
                      torch.zeros(pages, heads, dim, page, dtype=torch.int8, device=device),
                      torch.ones(pages, heads, device=device), torch.ones(pages, heads, device=device))
 
-    def q_heads_ok(self, n):
-        return n % self.heads == 0
-
 
 class Batch:
     """A batch of requests (palq_batch): table int32 [requests, max_pages],
@@ -436,7 +432,7 @@ class Batch:
             raise PalqError(ERR_ARG, "table must be contiguous int32")
         _need(lens, torch.int32, requests, "lens")
         _need(starts, torch.int32, requests + 1, "starts")
-        self.table, self.lens, self.starts = table, lens, starts
+        self.table, self.lens, self.starts, self.tokens = table, lens, starts, 0
         self.desc = BatchDesc(requests, max_pages, table.data_ptr(), lens.data_ptr(), starts.data_ptr(), 0, max_new, max_len)
         self.ref = ctypes.byref(self.desc)
 
@@ -448,25 +444,30 @@ def _need(t, dtype, n, what):
 
 def _rows2(t):
     """Type and row stride of a [rows, cols] tensor with consecutive columns."""
-    rows, cols = t.shape
     ld, one = t.stride()
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
+        raise PalqError(ERR_ARG, f"no element type for {t.dtype}")
+    rows, cols = t.shape
     if one != 1 and cols > 1:
         raise PalqError(ERR_ARG, "a row's elements must be consecutive")
-    if t.dtype not in _TYPES:
-        raise PalqError(ERR_ARG, f"no element type for {t.dtype}")
-    return _TYPES[t.dtype], (ld if rows > 1 else max(ld, cols))
+    return kind, (ld if rows > 1 else max(ld, cols))
 
 
-def _rows3(t, batch, cache, heads_ok=None):
-    """Type, row and head stride of a [tokens, heads, head_dim] tensor of a batch."""
-    tokens, heads, dim = t.shape
-    row, head, one = t.stride()
-    if one != 1 or dim != cache.dim or (heads != cache.heads if heads_ok is None else not heads_ok(heads)):
-        raise PalqError(ERR_ARG, "tensor must be [tokens, heads, head_dim] of the cache, a head's channels consecutive")
-    batch.desc.tokens = tokens
-    if t.dtype not in _TYPES:
-        raise PalqError(ERR_ARG, f"no element type for {t.dtype}")
-    return _TYPES[t.dtype], row, head
+def _pair3(a, b, batch, cache, query=False):
+    """Type, and row and head strides of both, of two [tokens, heads, head_dim]
+    tensors of a batch (query: of any multiple of the cache's heads)."""
+    tokens, heads, dim = a.shape
+    ar, ah, a1 = a.stride()
+    br, bh, b1 = b.stride()
+    kind = _TYPES.get(a.dtype)
+    if a.dtype != b.dtype or b.shape != a.shape or kind is None:
+        raise PalqError(ERR_ARG, "the tensors differ in type or shape, or have no element type of the library")
+    if a1 != 1 or b1 != 1 or dim != cache.dim or (heads % cache.heads if query else heads != cache.heads):
+        raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim] of the cache, a head's channels consecutive")
+    if batch.tokens != tokens:
+        batch.tokens = batch.desc.tokens = tokens
+    return kind, ar, ah, br, bh
 
 
 class ConvPlan:
