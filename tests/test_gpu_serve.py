@@ -74,6 +74,10 @@ def check_linear(got, q, s, w, ws, b, y_type):
     t = np.abs(S.linear(q, s, w, ws))
     bias = 0 if b is None else np.abs(b)
     tol = 5 * 2.0 ** -24 * (t + bias) + EPS[y_type] * 1.01 * np.abs(ref) + TINY[y_type]
+    if y_type == "f16":  # past its range: inf
+        over = np.abs(ref) >= 65520
+        assert (got[over] == np.copysign(np.inf, ref[over])).all()
+        got, ref, tol = got[~over], ref[~over], tol[~over]
     err = np.abs(got - ref)
     assert (err <= tol).all(), f"{(err > tol).sum()} of {err.size} off, worst {np.max(err / np.maximum(tol, 1e-300)):.3g} of the bound"
 
@@ -102,6 +106,29 @@ def test_linear(palq, x_type, y_type, rows, n_in, n_out):
     check_linear(host(y[:, :n_out]), q, s, w, ws, b, y_type)
     assert torch.equal(y[:, :n_out], y2)
     assert (host(y[:, n_out:]) == 7).all()
+
+
+@pytest.mark.parametrize("x_type,y_type", [("bf16", "bf16"), ("i8", "f32"), ("f32", "f16")])
+@pytest.mark.parametrize("rows,n_in,n_out,kernel", [(1, 200, 50, "one"), (1, 17000, 50, "few"), (15, 700, 90, "few"), (40, 700, 90, "few"),
+                                                    (70, 130, 8200, "tile"), (70, 1100, 8195, "tile"), (1100, 130, 3700, "tile"),
+                                                    (1090, 900, 3701, "tile"), (2100, 200, 3900, "tile"), (2051, 650, 3899, "tile"),
+                                                    (3300, 64, 3900, "tile"), (3329, 450, 3903, "tile")])
+def test_linear_every_kernel(palq, x_type, y_type, rows, n_in, n_out, kernel):
+    """Both sides of every size rule: one row, 16 and 32 rows of the few-row kernel, tiles of 64, 128 (two builds) and 256, with
+    k of one stage and of several, ends inside tiles."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("linear", x_type, y_type, rows, n_in, n_out, kernel)
+    g = np.random.default_rng(rows + n_in)
+    w, ws, b, x, s = linear_case(g, rows, n_in, n_out, x_type, True)
+    xt = dev(x, x_type)
+    lin = P.Linear(palq, dev(w), dev(ws), dev(b), max_rows=rows)
+    assert lin.kernels(rows) == f"linear_{kernel}_kernel"
+    y = torch.empty(rows, n_out, dtype=tdt(y_type), device="cuda")
+    lin.run(xt, y, x_scale=None if s is None else dev(s))
+    palq.sync()
+    q, s = (x, s) if x_type == "i8" else S.quantize_rows(host(xt))
+    check_linear(host(y), q, s, w, ws, b, y_type)
 
 
 def test_linear_strided_operands(palq):
@@ -359,16 +386,19 @@ def check_attend(pair, got, table, lens, starts, q, scale, dtype, **kw):
     assert (got[seen == 0] == 0).all()
 
 
-def attend_case(P, ctx, seed, dtype, page, dim, heads, group, lens, new, causal=True, window=0, spread=0.5, q_mul=1.5):
+def attend_case(P, ctx, seed, dtype, page, dim, heads, group, lens, new, causal=True, window=0, spread=0.5, q_mul=1.5, max_len=None,
+                missing=()):
     import torch
     g = np.random.default_rng(seed)
     table, pages = paged(g, lens, page)
+    for r, block in missing:
+        table[r, block] = -1 if r % 2 else pages
     pair = Pair(P, pages, heads, page, dim)
     pair.fill(g, table, lens, spread)
     starts = cumsum(new)
     q = dev(g.standard_normal((starts[-1], heads * group, dim)) * q_mul, dtype)
     out = torch.full_like(q, 3.0)
-    b = pair.batch(table, lens, starts)
+    b = pair.batch(table, lens, starts, max_len=max_len)
     ctx.attention(pair.gpu, q, out, b, dim ** -0.5, causal=causal, window=window)
     ctx.sync()
     check_attend(pair, host(out), table, lens, starts, host(q), dim ** -0.5, dtype, causal=causal, window=window)
@@ -408,6 +438,50 @@ def test_attention_many_rows(palq, dtype, page, dim, heads, group, lens, new, ca
     from paper_2208_01944_amd import palq as P
     say("attention rows", dtype, page, dim, heads, group, lens, new, causal, window)
     attend_case(P, palq, page * 3 + dim + group, dtype, page, dim, heads, group, lens, new, causal, window)
+
+
+# enough rows for the 128-row kernel: more than 768 blocks of 32 rows (16 for heads of 256)
+@pytest.mark.parametrize("dtype,page,dim,heads,group,lens,new,causal,window,max_len,missing", [
+    ("bf16", 64, 128, 16, 2, [128, 150, 131, 300, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120], True, 0, None, ()),
+    ("f16", 16, 64, 16, 2, [128, 150, 131, 300, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120], True, 50, None, ()),
+    ("bf16", 32, 96, 16, 2, [70, 150, 0, 1, 129, 64, 191], [131, 40, 5, 100, 1, 64, 120], False, 0, None, ()),
+    ("f16", 128, 256, 8, 1, [100, 150, 131, 20, 129, 64, 65, 191], [200, 40, 131, 70, 1, 64, 0, 120], True, 0, None, ()),
+    ("bf16", 64, 64, 16, 3, [160, 100, 130, 61, 200], [100, 100, 110, 100, 90], True, 0, 5000, ()),             # split, a part empty
+    ("f16", 16, 128, 16, 3, [1300, 100, 130, 700, 200], [60, 100, 20, 31, 100], True, 700, 4000, ()),           # split, windows
+    ("bf16", 16, 128, 16, 2, [128, 150, 131, 170, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120], True, 0, None, ((0, 0), (1, 3), (5, 12))),
+])
+def test_attention_tile_kernel(palq, dtype, page, dim, heads, group, lens, new, causal, window, max_len, missing):
+    from paper_2208_01944_amd import palq as P
+    say("attention tiles", dtype, page, dim, heads, group, lens, new, causal, window, max_len)
+    assert -(-max(new) * group // (16 if dim == 256 else 32)) * heads * len(lens) > 768
+    attend_case(P, palq, page + dim, dtype, page, dim, heads, group, lens, new, causal, window, max_len=max_len, missing=missing)
+
+
+def test_attention_tile_kernel_not_finite(palq):
+    """As test_attention_not_finite, on the 128-row kernel, with far scales and a negative score scale."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    g = np.random.default_rng(64)
+    page, dim, heads, lens, new = 16, 64, 16, [150, 128, 131, 100, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120]
+    table, pages = paged(g, lens, page)
+    pair = Pair(P, pages, heads, page, dim)
+    pair.fill(g, table, lens, 4.0)
+    spare = sorted(set(range(pages)) - set(table.ravel().tolist()))
+    pair.ref.ks[spare], pair.ref.vs[spare] = np.nan, np.inf
+    pair.ref.ks[table[0][9], 0] = np.nan   # tokens 144 on of request 0, head 0
+    pair.ref.vs[table[1][6], 1] = np.nan   # tokens 96 on of request 1, head 1
+    pair.upload()
+    starts = cumsum(new)
+    q = g.standard_normal((starts[-1], 2 * heads, dim)).astype(np.float32)
+    q[0, 0, 5], q[starts[1], 5, 3], q[starts[2], 7, 4] = np.nan, np.inf, -np.inf
+    qt = dev(q, "bf16")
+    out = torch.empty_like(qt)
+    for scale in (0.125, -0.2):
+        palq.attention(pair.gpu, qt, out, pair.batch(table, lens, starts), scale)
+        palq.sync()
+        with np.errstate(invalid="ignore"):
+            check_attend(pair, host(out), table, lens, starts, host(qt), scale, "bf16")
+        assert np.isnan(host(out)).any() and np.isfinite(host(out)).any()
 
 
 @pytest.mark.parametrize("rows", [1, 5, 20, 90])
@@ -608,6 +682,32 @@ def test_workspace_of_an_earlier_graph_stays(palq):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, ref)
+
+
+def test_capture_of_a_larger_shape_is_refused(palq):
+    """An attention whose workspace would have to grow while a graph is captured gives an error and leaves the capture whole."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    side = torch.cuda.Stream()
+    ctx = P.Context(0, stream=side.cuda_stream)
+    c = P.Cache.empty(80, 1, 64, 64)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    b = P.Batch(torch.arange(80, dtype=torch.int32, device="cuda")[None], i32(5000), i32(0, 1), 1, 5120)
+    q = torch.ones(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    out, y = torch.empty_like(q), torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        with pytest.raises(P.PalqError) as e:
+            ctx.attention(c, q, out, b, 1.0)
+        y.add_(1.0)
+    assert e.value.status == P.ERR_NOMEM
+    graph.replay()
+    torch.cuda.synchronize()
+    assert (y.cpu() == 1).all()
+    ctx.attention(c, q, out, b, 1.0)
+    ctx.sync()
+    assert (host(out) == 0).all()
 
 
 def test_empty_calls(palq):
