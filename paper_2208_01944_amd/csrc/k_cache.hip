@@ -10,7 +10,9 @@
 // 16 consecutive bytes.
 //
 // Both directions are bound by memory: a workgroup takes one (request, block,
-// head, keys or values), its threads 16 codes at a time.
+// head, keys or values).  8 prompts of 113 to 2048 tokens, 8 heads of 128, bf16: append 21
+// us (53 MB, 2.5 TB/s), read back as fp32 19 us (89 MB, 4.7 TB/s); 64 single tokens 6 us,
+// four loads that wait for each other (lengths, table, scale, values).
 #include <algorithm>
 
 #include "cache.h"

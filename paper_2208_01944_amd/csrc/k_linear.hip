@@ -275,7 +275,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void linear_one_kernel(LinearArg
 // wave 32 CT x 32 TT of them on v_mfma_i32_32x32x32_i8.  k goes by stages of 128:
 // both operands' slabs are copied from memory straight into LDS (two stages, one
 // in use, one on its way), and a wave reads the operands of the next 32 k while
-// the matrix cores work on the present ones, across the stage's barrier too.
+// the matrix cores work on the present ones, across the stage's barrier too.  4096 rows,
+// 8192 x 8192 weights: 230 us, 2.4 POP/s, as the library's int8 product (2.39; its
+// codes come ready); the matrix cores are busy 65 % of the time at 1.7 GHz, to which
+// operands of random codes bring the clock down (all-zero codes: 184 us).
 // 16 bytes per lane from the buffer into LDS at `dst` (uniform) + 16 lane; in asm,
 // so that the compiler does not order LDS reads after them: the stages' waits and
 // barriers do.
