@@ -25,12 +25,19 @@ struct palq_linear {
 
 namespace {
 
+// (no exception leaves the library: without memory for the text the status stands alone)
 palq_status fail(palq_ctx *ctx, palq_status code, const char *msg) {
-  ctx->err = msg;
+  try {
+    ctx->err = msg;
+  } catch (...) {
+  }
   return code;
 }
 palq_status device_fail(palq_ctx *ctx, hipError_t e, const char *what) {
-  ctx->err = std::string(what) + ": " + hipGetErrorString(e);
+  try {
+    ctx->err = std::string(what) + ": " + hipGetErrorString(e);
+  } catch (...) {
+  }
   return PALQ_ERR_DEVICE;
 }
 
