@@ -395,7 +395,7 @@ __device__ __forceinline__ void ahead() {
   __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
 
-template <class T, int D>
+template <class T, int D, bool WIDE>
 __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
   typedef TileLds<D> G;
   constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + 255) / 256;
@@ -461,12 +461,22 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   auto none = [&](int i) __attribute__((always_inline)) { return 4 * D % 256 && (int)threadIdx.x + i * 256 >= 4 * D; };
   // Table entries go through two sets of registers by the tile's parity (a copy from
   // one to the other would wait for them, and so for every load before them).
-  struct Entries { int k[PP], v[PP], b; } ent[2];
+  // WIDE (pages of a tile or more): the entries are the same for all threads and stay in
+  // scalar registers, as do the pages' addresses.
+  struct Entries { int k[WIDE ? 1 : PP], v[WIDE ? 1 : PP], b; } ent[2];
   v4i kx[PP], vx[PP];
   float bks, bvs, bthere;  // of chunk threadIdx.x % 4 of tile p
   const uint32_t page_bytes = (uint32_t)heads << cv.shift;  // (times D)
   const int8_t *kh = cv.k + ((int64_t)h << cv.shift) * D, *vh = cv.v + ((int64_t)h << cv.shift) * D;
+  typedef const __attribute__((address_space(4))) int32_t *ScalarInts;
+  typedef const __attribute__((address_space(4))) float *ScalarFloats;
   auto entries = [&](int p, Entries &e) __attribute__((always_inline)) {
+    if constexpr (WIDE) {
+      const ScalarInts st = (ScalarInts)(uintptr_t)table;
+      e.k[0] = e.b = st[__builtin_amdgcn_readfirstlane((uint32_t)min(p * 64, hi - 1) >> cv.shift)];
+      e.v[0] = st[__builtin_amdgcn_readfirstlane((uint32_t)min(max(p - 1, tb) * 64, hi - 1) >> cv.shift)];
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
       e.k[i] = entry(p * 64 + piece(i).tok);
@@ -476,6 +486,21 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   };
   auto load = [&](int p, const Entries &e) __attribute__((always_inline)) {
     const int ktile = p * 64 & pm, vtile = max(p - 1, tb) * 64 & pm;  // of a page that is wider than a tile
+    if constexpr (WIDE) {
+      const int kp = __builtin_amdgcn_readfirstlane(valid(e.k[0]) ? e.k[0] : 0), vp = __builtin_amdgcn_readfirstlane(valid(e.v[0]) ? e.v[0] : 0);
+      const int8_t *kt = kh + (uint64_t)kp * page_bytes * D + ktile * D, *vt = vh + (uint64_t)vp * page_bytes * D + vtile;
+#pragma unroll
+      for (int i = 0; i < PP; ++i) {
+        const Piece pc = piece(i);
+        kx[i] = *(const v4i *)(kt + (uint32_t)(pc.tok * D + pc.s * 16));
+        vx[i] = *(const v4i *)(vt + (uint32_t)((pc.d << cv.shift) + pc.vt));
+      }
+      const int64_t at = (int64_t)kp * heads + h;
+      bks = ((ScalarFloats)(uintptr_t)cv.ks)[at];
+      bvs = ((ScalarFloats)(uintptr_t)cv.vs)[at];
+      bthere = valid(e.b) ? 1.0f : 0.0f;
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
       const Piece pc = piece(i);
@@ -747,7 +772,9 @@ template <class T, int D>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
   if (a.block == 128) {
-    attend_tile_kernel<T, D><<<(unsigned)(rt * a.splits * a.c.heads * a.b.requests), 256, 0, s>>>(a, (int)rt);
+    const unsigned flat = (unsigned)(rt * a.splits * a.c.heads * a.b.requests);
+    if (a.c.page >= 64) attend_tile_kernel<T, D, true><<<flat, 256, 0, s>>>(a, (int)rt);
+    else attend_tile_kernel<T, D, false><<<flat, 256, 0, s>>>(a, (int)rt);
   } else {
     const dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
     if (a.block == 16) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
