@@ -359,7 +359,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 // as codes a tile ahead, converted to fp16 once and kept in LDS for all waves, one
 // barrier a tile; two workgroups on a CU (up to 128 channels) fill each other's gaps.
 // 4 requests, 1531 to 2048 tokens behind cached ones, 2100 to 4096 in all, 8 heads of
-// 128, group 4: 328 us, 755 TFLOP/s (a bf16 library product of 8192^3: 1240).  A wave's
+// 128, group 4: 320 us, 775 TFLOP/s (a bf16 library product of 8192^3: 1240).  A wave's
 // step of 64 tokens takes about 4000 cycles alone, 1024 of them products; without the
 // softmax the time falls by 7 %, without the conversion by 27 %.
 //
