@@ -471,7 +471,8 @@ void launch_few(const LinearArgs &a, hipStream_t s) {
 // The kernel for this many rows and channels.  The largest tile that still gives
 // (nearly) every CU one: operands are then read least often.  Measured with the
 // quantiser, bf16, 4096 x 4096 weights: 64 rows 9.7 us on linear_few, 14.6 on 64 x 64
-// tiles; 512 rows 22.3 on 64 x 64, 25.0 on 128 x 128; 1024 rows (a 128 x 128 tile a CU) 29.3
+// tiles, 192 rows (192 tiles) 15 on either, 304 rows of 7296 to 3200 channels (250 tiles) 35
+// and 25; 512 rows 22.3 on 64 x 64, 25.0 on 128 x 128; 1024 rows (a 128 x 128 tile a CU) 29.3
 // with 8 waves and 4 stages of 128 k, 32.6 with 4 waves and 3 of 64, which lets three stand
 // on a CU: 2048 rows 50 and 55; 4096 rows 79 on 256 x 256, 94 on 128 x 128.
 enum LinearKind { kFew1, kFew2, kTile64, kTile128, kTile128Many, kTile256 };
@@ -480,7 +481,7 @@ LinearKind linear_kind(int64_t rows, int n_out) {
   if (tiles(256) >= 192) return kTile256;
   if (tiles(128) >= 512) return kTile128Many;
   if (tiles(128) >= 256) return kTile128;
-  if (rows > 32 && tiles(64) >= 256) return kTile64;
+  if (rows > 32 && tiles(64) >= 160) return kTile64;
   return rows > 16 ? kFew2 : kFew1;
 }
 
