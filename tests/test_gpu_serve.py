@@ -529,6 +529,34 @@ def test_attention_not_finite(palq):
         assert np.isnan(host(out)).any() and np.isfinite(host(out)).any()
 
 
+@pytest.mark.parametrize("scale", [0.125, -0.125, 0.0])
+@pytest.mark.parametrize("dim,group,new", [(64, 1, [2, 17, 20]), (64, 3, [1, 1, 1]), (96, 2, [3, 1, 9]), (128, 4, [1, 1, 3]),
+                                           (128, 8, [3, 4, 4]), (256, 2, [1, 7, 2])])
+def test_attention_whole_tiles(palq, dim, group, new, scale):
+    """Few rows over several tiles that all of them see, between tiles that some of them see: scales of either sign and
+    none, a key and a value block with a NaN scale in such a tile."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("attention whole tiles", dim, group, scale)
+    g = np.random.default_rng(65 + dim + group)
+    page, lens = 16, [650, 400, 129]
+    table, pages = paged(g, lens, page)
+    pair = Pair(P, pages, 2, page, dim)
+    pair.fill(g, table, lens)
+    pair.ref.ks[table[1][9], 0] = np.nan   # tokens 144 on of request 1, head 0
+    pair.ref.vs[table[2][5], 1] = np.nan   # tokens 80 on of request 2, head 1
+    pair.upload()
+    starts = cumsum(new)
+    q = dev(g.standard_normal((starts[-1], 2 * group, dim)) * 1.5, "f16")
+    out = torch.empty_like(q)
+    for kw in ({"causal": True}, {"causal": True, "window": 200}, {"causal": False}):
+        palq.attention(pair.gpu, q, out, pair.batch(table, lens, starts), scale, **kw)
+        palq.sync()
+        with np.errstate(invalid="ignore"):
+            check_attend(pair, host(out), table, lens, starts, host(q), scale, "f16", **kw)
+        assert np.isfinite(host(out)).any()
+
+
 def test_attention_strided(palq):
     """q inside a fused row, out with its heads apart, odd element offsets."""
     import torch
