@@ -16,6 +16,7 @@
 #include <algorithm>
 
 #include "cache.h"
+#include "cache_index.h"
 #include "serve_common.h"
 
 namespace palq {
@@ -53,10 +54,10 @@ struct NewKv {
 // NI items a thread hold a whole block in registers, so new values are read once.
 // Values are turned (a word of 4 tokens for each channel) through LDS.
 template <class T, int NI>
-__global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchView b, NewKv x) {
+__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView c, BatchView b, NewKv x) {
   typedef typename T::raw R;
   __shared__ uint32_t part[4];
-  __shared__ uint32_t turned[NI * 2048 + 256];  // [dim][page / 4 + 1] words
+  __shared__ uint32_t turned[turned_words(NI)];  // [dim][turned_stride]
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
   const Request q = request_of(b, r, c.shift);
@@ -66,7 +67,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   if (lo >= hi) return;
   const int pid = page_of(c, b, r, block);
   if (pid < 0) return;
-  const int kept = lo - t0, end = hi - t0, D = c.dim, groups = D / 8, items = c.page / 4 * groups;
+  const int kept = lo - t0, end = hi - t0, D = c.dim, groups = D / 8, items = append_items(c.page, D);
   const R *src = (const R *)(values ? x.v : x.k);
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
   src += (q.row0 + (t0 - (q.len - q.n))) * row + h * head;  // row of token t0 (there may be none)
@@ -78,7 +79,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   uint32_t mag = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int p = threadIdx.x + i * 256, tq = p / groups * 4, ch = p % groups * 8;
+    const int p = threadIdx.x + i * kAppendThreads, tq = p / groups * 4, ch = p % groups * 8;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const bool here = p < items && tq + t >= kept && tq + t < end;
@@ -105,10 +106,10 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   const bool bad = !(s == s), grown = kept && !bad && s > had;
   if (threadIdx.x == 0) *scale = s;
   int8_t *dst = (values ? c.v : c.k) + ph * c.page * D;
-  const int words = c.page / 4 + 1;
+  const int words = turned_stride(c.page);
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
-    const int p = threadIdx.x + i * 256, tq = p / groups * 4, ch = p % groups * 8;
+    const int p = threadIdx.x + i * kAppendThreads, tq = p / groups * 4, ch = p % groups * 8;
     if (p >= items || tq + 4 <= kept || tq >= end) continue;
     uint32_t w[4][2];  // codes of a token's 8 channels
 #pragma unroll
@@ -134,14 +135,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheView c, BatchVie
   }
   if (!values) {
     if (grown)
-      for (int p = threadIdx.x; p < kept * (D / 16); p += 256) ((v4i *)dst)[p] = rescale16(((const v4i *)dst)[p], ratio);
+      for (int p = threadIdx.x; p < kept * (D / 16); p += kAppendThreads) ((v4i *)dst)[p] = rescale16(((const v4i *)dst)[p], ratio);
     return;
   }
   __syncthreads();
   // a piece: 16 tokens of one channel; where old ones are among them, or all are and the
   // scale grew, what is there comes first
   const int c0 = grown ? 0 : kept >> 4, pieces = ((end + 15) >> 4) - c0;
-  for (int p = threadIdx.x; p < pieces * D; p += 256) {
+  for (int p = threadIdx.x; p < pieces * D; p += kAppendThreads) {
     const int d = p / pieces, at = (c0 + p % pieces) * 16;
     int8_t *to = dst + d * c.page;
     if (at < kept && !grown) {  // only what is new: the old codes need not come first
@@ -230,13 +231,12 @@ unsigned blocks_of(const CacheView &c, const BatchView &b) {
   return (unsigned)std::min<int64_t>((n + c.page - 2) / c.page + 1, b.max_pages);
 }
 
-// Items of a thread: a block of page x dim elements, 32 an item, 256 threads.
 template <class T>
 void launch_append_t(dim3 g, const CacheView &c, const BatchView &b, const NewKv &x, hipStream_t s) {
-  const int n = c.page * c.dim / 8192;
-  if (n <= 1) cache_append_kernel<T, 1><<<g, 256, 0, s>>>(c, b, x);
-  else if (n <= 2) cache_append_kernel<T, 2><<<g, 256, 0, s>>>(c, b, x);
-  else cache_append_kernel<T, 4><<<g, 256, 0, s>>>(c, b, x);
+  const int n = append_rounds(c.page, c.dim);
+  if (n == 1) cache_append_kernel<T, 1><<<g, kAppendThreads, 0, s>>>(c, b, x);
+  else if (n == 2) cache_append_kernel<T, 2><<<g, kAppendThreads, 0, s>>>(c, b, x);
+  else cache_append_kernel<T, 4><<<g, kAppendThreads, 0, s>>>(c, b, x);
 }
 
 }  // namespace

@@ -1,0 +1,43 @@
+"""GPU checks of the 8-bit transformer operators over every page and head size that
+they take, and at the edges of their ranges, against the numpy oracle."""
+import numpy as np
+import pytest
+
+from oracle import serve as S  # noqa: F401
+from tests.test_gpu_serve import Pair, attend_case, check_attend, cumsum, dev, host, paged, say, tdt  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+PAIRS = [(page, dim) for page in (16, 32, 64, 128) for dim in (64, 96, 128, 256)]
+
+
+@pytest.mark.parametrize("page,dim", PAIRS)
+def test_append_and_read_every_size(palq, page, dim):
+    """Whole blocks, parts of blocks and single tokens, new and behind others, in every page and head size: codes and scales
+    equal to the oracle's, values that grow so that old codes are rescaled."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("append sizes", page, dim)
+    g = np.random.default_rng(page * 7 + dim)
+    heads, steps = 2, [[page, 1, 3 * page // 4, 2 * page + 3], [1, page - 1, page // 4 + 1, page], [page + 2, 3, 1, page - 5]]
+    final = np.sum(steps, 0)
+    table, pages = paged(g, final.tolist(), page)
+    pair = Pair(P, pages, heads, page, dim)
+    pair.fill(g, table, final)
+    lens = np.zeros(4, int)
+    for i, new in enumerate(steps):
+        lens = lens + new
+        starts = cumsum(new)
+        k, v = (dev(g.standard_normal((starts[-1], heads, dim)) * np.exp(g.standard_normal((starts[-1], heads, dim)) + i), "bf16")
+                for _ in range(2))
+        pair.ref.append(table, lens.tolist(), starts, host(k), host(v))
+        palq.cache_append(pair.gpu, k, v, pair.batch(table, lens.tolist(), starts))
+        palq.sync()
+        pair.check(table, lens.tolist())
+    starts = cumsum(lens.tolist())
+    k, v = torch.zeros(starts[-1], heads, dim, device="cuda"), torch.zeros(starts[-1], heads, dim, device="cuda")
+    palq.cache_read(pair.gpu, k, v, pair.batch(table, lens.tolist(), starts))
+    palq.sync()
+    rk, rv = pair.ref.read(table, lens.tolist(), starts)
+    np.testing.assert_array_equal(host(k), rk)
+    np.testing.assert_array_equal(host(v), rv)
