@@ -31,6 +31,7 @@
 #include <type_traits>
 
 #include "cache.h"
+#include "cache_index.h"
 
 namespace palq {
 
@@ -412,7 +413,7 @@ __device__ __forceinline__ void ahead() {
 template <class T, int D, bool WIDE>
 __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
   typedef TileLds<D> G;
-  constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + 255) / 256;
+  constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + kTileThreads - 1) / kTileThreads;
   __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
   __shared__ float4 blocks[4][4];  // of four tiles' 16-token chunks: {ks, log2 vs, 1 / vs, page there}
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, c = lane >> 5;
@@ -467,12 +468,8 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   auto valid = [&](int pid) __attribute__((always_inline)) { return (uint32_t)pid < (uint32_t)cv.pages; };
   // The 16-byte pieces that this thread brings: 16 channels of a key of tile p and 16
   // tokens of a value channel of tile p - 1.
-  struct Piece { int tok, s, kr, d, vt; };  // key's token, 16 channels, matrix row; value's channel, first token
-  auto piece = [&](int i) __attribute__((always_inline)) {
-    const int p = threadIdx.x + i * 256, j = p & 7, s = p / 8 % KS, gu = p / (8 * KS), g = gu & 3, u = gu >> 2;
-    return Piece{u * 32 + (j >> 2) * 16 + g * 4 + (j & 3), s, u * 32 + g * 8 + j, (p >> 6) * 16 + (p & 15), (p >> 4 & 3) * 16};
-  };
-  auto none = [&](int i) __attribute__((always_inline)) { return 4 * D % 256 && (int)threadIdx.x + i * 256 >= 4 * D; };
+  auto piece = [&](int i) __attribute__((always_inline)) { return tile_piece((int)threadIdx.x + i * kTileThreads, D); };
+  auto none = [&](int i) __attribute__((always_inline)) { return tile_piece_past((int)threadIdx.x + i * kTileThreads, D); };
   // Table entries go through two sets of registers by the tile's parity (a copy from
   // one to the other would wait for them, and so for every load before them).
   // WIDE (pages of a tile or more): the entries are the same for all threads and stay in
@@ -502,12 +499,12 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     const int ktile = p * 64 & pm, vtile = max(p - 1, tb) * 64 & pm;  // of a page that is wider than a tile
     if constexpr (WIDE) {
       const int kp = __builtin_amdgcn_readfirstlane(valid(e.k[0]) ? e.k[0] : 0), vp = __builtin_amdgcn_readfirstlane(valid(e.v[0]) ? e.v[0] : 0);
-      const int8_t *kt = kh + (uint64_t)kp * page_bytes * D + ktile * D, *vt = vh + (uint64_t)vp * page_bytes * D + vtile;
+      const int8_t *kt = kh + (uint64_t)kp * page_bytes * D, *vt = vh + (uint64_t)vp * page_bytes * D;
 #pragma unroll
       for (int i = 0; i < PP; ++i) {
-        const Piece pc = piece(i);
-        kx[i] = *(const v4i *)(kt + (uint32_t)(pc.tok * D + pc.s * 16));
-        vx[i] = *(const v4i *)(vt + (uint32_t)((pc.d << cv.shift) + pc.vt));
+        const TilePiece pc = piece(i);
+        kx[i] = *(const v4i *)(kt + tile_key_at(pc, ktile, 63, D));
+        vx[i] = *(const v4i *)(vt + tile_value_at(pc, vtile, 63, cv.shift));
       }
       const int64_t at = (int64_t)kp * heads + h;
       bks = ((ScalarFloats)(uintptr_t)cv.ks)[at];
@@ -517,11 +514,11 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     }
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
-      const Piece pc = piece(i);
+      const TilePiece pc = piece(i);
       const uint64_t kp = (uint64_t)(uint32_t)(valid(e.k[i]) ? e.k[i] : 0) * page_bytes * D;
       const uint64_t vp = (uint64_t)(uint32_t)(valid(e.v[i]) ? e.v[i] : 0) * page_bytes * D;
-      kx[i] = *(const v4i *)(kh + kp + (uint32_t)((ktile + (pc.tok & pm)) * D + pc.s * 16));
-      vx[i] = *(const v4i *)(vh + vp + (uint32_t)((pc.d << cv.shift) + vtile + (pc.vt & pm)));
+      kx[i] = *(const v4i *)(kh + kp + tile_key_at(pc, ktile, pm, D));
+      vx[i] = *(const v4i *)(vh + vp + tile_value_at(pc, vtile, pm, cv.shift));
     }
     const bool page = valid(e.b);
     const int64_t at = (int64_t)(page ? e.b : 0) * heads + h;
@@ -543,7 +540,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
       if (none(i)) break;
-      const Piece pc = piece(i);
+      const TilePiece pc = piece(i);
       // operand (subtile, 16 channels): lane 32 c + row has 8 channels from 8 c
       uint8_t *kd = kbase + ((pc.kr >> 5) * KS + pc.s) * 1024 + (pc.kr & 31) * 16;
       *(h8 *)kd = codes_h8((uint32_t)kx[i][0], (uint32_t)kx[i][1]);

@@ -45,3 +45,39 @@ def test_append_takes_every_value_of_a_block(append_shapes, page, dim):
                 assert all(0 <= (channels + j) * stride + tokens // 4 < words for j in range(8))
     assert seen == {(t, c) for t in range(page) for c in range(dim)}
     assert (dim - 1) * stride + (page - 1) // 4 < words  # the last word read back
+
+
+@pytest.fixture(scope="module")
+def tile_shapes(tmp_path_factory):
+    """{dim: pieces} and {(page, dim): offsets} of attend_tile_kernel's loads, thread after thread, for every tile of a page."""
+    rows = evaluate(tmp_path_factory.mktemp("tile"), """
+  for (int shift = 4; shift <= 7; ++shift)
+    for (int dim : kDims)
+      for (int tile = 0; tile == 0 || tile < 1 << shift; tile += 64)
+        for (int n = 0; n < (4 * dim + kTileThreads - 1) / kTileThreads * kTileThreads; ++n) {
+          const int page = 1 << shift, mask = page < 64 ? page - 1 : 63;
+          const TilePiece p = tile_piece(n, dim);
+          std::printf("%d %d %d %d %u %u %d %d %d %d %d\\n", page, dim, n, tile_piece_past(n, dim), tile_key_at(p, tile, mask, dim),
+                      tile_value_at(p, tile, mask, shift), p.tok, p.s, p.kr, p.d, p.vt);
+        }""")
+    out = {}
+    for r in rows:
+        out.setdefault((r[0], r[1]), []).append(r[2:])
+    assert sorted(out) == PAIRS
+    return out
+
+
+@pytest.mark.parametrize("page,dim", PAIRS)
+def test_tile_loads_stay_inside_a_block(tile_shapes, page, dim):
+    """Loads of every thread, those without a piece among them, lie in the block of page x dim bytes; the pieces that count
+    are the whole tile, each once, and each key piece has a place of its own."""
+    block = page * dim
+    for n, past, key, value, *_ in tile_shapes[page, dim]:
+        assert 0 <= key <= block - 16 and 0 <= value <= block - 16, n
+    tiles = max(1, page // 64)
+    real = [r for r in tile_shapes[page, dim] if not r[1]]
+    assert len(real) == 4 * dim * tiles
+    real = real[:4 * dim]
+    assert {(tok, s) for *_, tok, s, kr, d, vt in real} == {(t, s) for t in range(64) for s in range(dim // 16)}
+    assert {(kr, s) for *_, tok, s, kr, d, vt in real} == {(t, s) for t in range(64) for s in range(dim // 16)}
+    assert {(d, vt) for *_, tok, s, kr, d, vt in real} == {(d, t) for d in range(dim) for t in range(0, 64, 16)}

@@ -41,3 +41,23 @@ def test_append_and_read_every_size(palq, page, dim):
     rk, rv = pair.ref.read(table, lens.tolist(), starts)
     np.testing.assert_array_equal(host(k), rk)
     np.testing.assert_array_equal(host(v), rv)
+
+
+@pytest.mark.parametrize("page,dim", PAIRS)
+def test_attention_tiles_every_size(palq, page, dim):
+    """The 128-row kernel in every page and head size, rows and tokens that end inside tiles."""
+    from paper_2208_01944_amd import palq as P
+    say("attention tiles, sizes", page, dim)
+    lens, new, heads, group = [128, 150, 131, 260, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120], 16, 2
+    assert -(-max(new) * group // (16 if dim == 256 else 32)) * heads * len(lens) > 768
+    for causal, window in ((True, 0), (True, 70), (False, 0)):
+        attend_case(P, palq, page * 5 + dim, "bf16", page, dim, heads, group, lens, new, causal, window)
+
+
+@pytest.mark.parametrize("page,dim", PAIRS)
+def test_attention_rows_every_size(palq, page, dim):
+    """The kernels of 16 and 32 rows in every page and head size."""
+    from paper_2208_01944_amd import palq as P
+    say("attention rows, sizes", page, dim)
+    for lens, new, group, window in (([1, 130, 64, 300], [1, 1, 1, 1], 4, 0), ([9, 130, 200], [9, 11, 5], 3, 50)):
+        attend_case(P, palq, page * 3 + dim, "f16", page, dim, 2, group, lens, new, True, window)
