@@ -512,7 +512,8 @@ typedef struct {
  *   (they size the launches; closer bounds run faster).
  * Device values outside these bounds never lead outside the tensors: rows
  * past max_new and tokens past max_len or the table are left out, as are
- * tokens on a page number outside [0, pages). */
+ * tokens on a page number outside [0, pages).  What is left out does not move
+ * the rest: a row's position follows from lens and starts as they are. */
 typedef struct {
   int32_t requests, max_pages;
   const int32_t *table, *lens, *starts;
@@ -532,7 +533,9 @@ typedef struct {
 palq_status palq_cache_append(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *k, int64_t k_row,
                               int64_t k_head, const void *v, int64_t v_row, int64_t v_head, int32_t type);
 /* The inverse: code * scale of each request's last tokens, to tensors laid
- * out as in palq_cache_append; 0 for tokens on pages out of range. */
+ * out as in palq_cache_append; 0 for tokens on pages out of range.  Rows that
+ * are left out, or whose position is none of the request's (before 0, or past
+ * max_len or the table), stay as they are. */
 palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, void *k, int64_t k_row,
                             int64_t k_head, void *v, int64_t v_row, int64_t v_head, int32_t type);
 
@@ -545,7 +548,7 @@ palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_b
  * own position, with window > 0 only the last `window` of them; with
  * causal = 0 all (cross attention to cached encoder states: the rows then
  * have no position, and may outnumber the tokens).  A row that sees no token
- * gives 0.  Scores, softmax and sums are fp32; probabilities enter the second
+ * gives 0; rows past max_new stay as they are.  Scores, softmax and sums are fp32; probabilities enter the second
  * product in fp16.  Long caches of few rows are split and joined in the
  * context's workspace, which may grow (never while a graph is captured:
  * PALQ_ERR_NOMEM then; run the shape once before).  out and q (address ranges)

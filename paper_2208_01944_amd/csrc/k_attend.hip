@@ -62,7 +62,7 @@ constexpr float kSlack = 8.0f;
 // One row's reach: tokens [lo, hi).
 struct Reach { int lo, hi; };
 __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Request &q, int t) {
-  const int pos = q.len - q.n + t;
+  const int pos = q.pos + t;
   Reach s{0, q.len};
   if (a.causal) {
     s.hi = max(0, min(q.len, pos + 1));

@@ -61,16 +61,16 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView 
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
   const Request q = request_of(b, r, c.shift);
-  const int old = max(0, q.len - q.n);  // rows before position 0 have no place
+  const int old = max(0, q.pos);  // rows before position 0 have no place
   const int block = (old >> c.shift) + (int)blockIdx.x;
-  const int t0 = block << c.shift, lo = max(old, t0), hi = min(q.len, t0 + c.page);
+  const int t0 = block << c.shift, lo = max(old, t0), hi = min(min(q.len, q.pos + q.n), t0 + c.page);
   if (lo >= hi) return;
   const int pid = page_of(c, b, r, block);
   if (pid < 0) return;
   const int kept = lo - t0, end = hi - t0, D = c.dim, groups = D / 8, items = append_items(c.page, D);
   const R *src = (const R *)(values ? x.v : x.k);
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
-  src += (q.row0 + (t0 - (q.len - q.n))) * row + h * head;  // row of token t0 (there may be none)
+  src += (q.row0 + ((int64_t)t0 - q.pos)) * row + h * head;  // row of token t0 (there may be none)
   const int64_t ph = (int64_t)pid * c.heads + h;
   float *scale = (values ? c.vs : c.ks) + ph;
   const float had = kept ? *scale : 0.0f;
@@ -174,16 +174,16 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
   const Request q = request_of(b, r, c.shift);
-  const int first = max(0, q.len - q.n);
+  const int first = max(0, q.pos);
   const int block = (first >> c.shift) + (int)blockIdx.x;
-  const int t0 = block << c.shift, lo = max(first, t0), hi = min(q.len, t0 + c.page);
+  const int t0 = block << c.shift, lo = max(first, t0), hi = min(min(q.len, q.pos + q.n), t0 + c.page);
   if (lo >= hi) return;
   const int pid = page_of(c, b, r, block), D = c.dim;
   const int64_t ph = (int64_t)max(pid, 0) * c.heads + h;
   const float s = pid < 0 ? 0.0f : (values ? c.vs : c.ks)[ph];
   const int8_t *src = (values ? c.v : c.k) + ph * c.page * D;
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
-  R *dst = (R *)(values ? x.v : x.k) + (q.row0 + (lo - (q.len - q.n))) * row + h * head;
+  R *dst = (R *)(values ? x.v : x.k) + (q.row0 + ((int64_t)lo - q.pos)) * row + h * head;
   // several pieces' loads in flight before the first store
   if (!values) {
     const int quads = D / 4, all = (hi - lo) * quads;

@@ -137,22 +137,20 @@ struct BatchView {
   int64_t tokens, max_len;
 };
 
-// Tokens of one request: `n` ragged rows from row0 on, its last positions
-// [len - n, len).  Whatever the arrays hold, len stays inside the table and the
-// rows inside the tensors.
-struct Request { int64_t row0; int32_t n, len; };
+// One request: `n` ragged rows from row0 on, at positions pos, pos + 1, .., and `len`
+// tokens.  Whatever the arrays hold, len stays inside the table and the rows
+// inside the tensors; what is left out (rows or tokens past the bounds) does not
+// move the others, so pos follows from lens and starts as they are.
+struct Request { int64_t row0; int32_t n, len, pos; };
 __device__ __forceinline__ Request request_of(const BatchView &b, int r, int shift) {
   Request q;
-  const int64_t s0 = b.starts[r], s1 = b.starts[r + 1];
-  q.row0 = s0 < 0 ? 0 : s0;
-  int64_t n = (s1 < b.tokens ? s1 : b.tokens) - q.row0;
-  if (n > b.max_new) n = b.max_new;
-  q.n = (int32_t)(n < 0 ? 0 : n);
-  int64_t len = b.lens[r];
-  const int64_t room = (int64_t)b.max_pages << shift;
-  if (len > room) len = room;
-  if (len > b.max_len) len = b.max_len;
-  q.len = (int32_t)(len < 0 ? 0 : len);
+  const int64_t s0 = b.starts[r], s1 = b.starts[r + 1], all = b.lens[r];
+  const int64_t skip = s0 < 0 ? -s0 : 0;  // rows before the tensors' first
+  q.row0 = s0 + skip;
+  const int64_t pos = all - (s1 - s0) + skip;
+  q.pos = (int32_t)min(max(pos, (int64_t)-0x7fffffff), (int64_t)0x7fffffff);  // (no row reaches 0 from the one end, there are none at the other)
+  q.n = (int32_t)max((int64_t)0, min(min(s1, b.tokens) - q.row0, b.max_new - skip));
+  q.len = (int32_t)max((int64_t)0, min(all, min((int64_t)b.max_pages << shift, b.max_len)));
   return q;
 }
 

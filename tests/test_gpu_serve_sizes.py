@@ -61,3 +61,110 @@ def test_attention_rows_every_size(palq, page, dim):
     say("attention rows, sizes", page, dim)
     for lens, new, group, window in (([1, 130, 64, 300], [1, 1, 1, 1], 4, 0), ([9, 130, 200], [9, 11, 5], 3, 50)):
         attend_case(P, palq, page * 3 + dim, "f16", page, dim, 2, group, lens, new, True, window)
+
+
+# lens, rows of the request, bounds: the position of its first row in the tensors, and how many rows are in both bounds
+LEFT_OUT = [
+    ("one past the table", 33, (0, 1), {}, 32, 1),
+    ("rows past the table", 34, (0, 3), {}, 31, 3),
+    ("past max_len", 23, (0, 5), dict(max_len=20), 18, 5),
+    ("rows past max_new", 30, (0, 5), dict(max_new=3), 25, 3),
+    ("rows past the tensors", 30, (0, 9), dict(max_new=9), 21, 6),
+    ("starts below 0", 30, (-2, 3), dict(max_new=5), 27, 3),
+    ("more rows than tokens", 2, (0, 5), {}, -3, 5),
+]
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("what,length,rows,bounds,pos,n", LEFT_OUT, ids=[c[0] for c in LEFT_OUT])
+def test_rows_left_out_move_no_others(palq, what, length, rows, bounds, pos, n, dim):
+    """Rows and tokens past the bounds are left out, and the others keep their positions: append, read and attention
+    of a request beside an ordinary one, six rows in the tensors."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("left out", what, dim)
+    g = np.random.default_rng(length)
+    page, heads, tokens = 16, 2, 6
+    table, room = np.int32([[3, 1]]), 32
+    top = min(room, bounds.get("max_len", room), length)  # its tokens
+    pair = Pair(P, 4, heads, page, dim)
+    pair.fill(g, table, None)
+    b = P.Batch(dev(table), dev(np.int32([length])), dev(np.int32(rows)), bounds.get("max_new", rows[1] - rows[0]), bounds.get("max_len", 64))
+    x, y = (g.standard_normal((tokens, heads, dim)).astype(np.float32) for _ in range(2))
+    # what is left: tensor row i at position first + i, for i in [0, n), of which those in [0, top) have a place
+    first, end = pos - rows[0] if rows[0] > 0 else pos, min(pos + n, top)
+    live = [i for i in range(n) if 0 <= first + i < end]
+    if live:
+        part = slice(live[0], live[-1] + 1)
+        pair.ref.append(table, [first + live[-1] + 1], [0, len(live)], x[part], y[part])
+    before = [t.clone() for t in (pair.gpu.k, pair.gpu.v, pair.gpu.k_scale, pair.gpu.v_scale)]
+    palq.cache_append(pair.gpu, dev(x), dev(y), b)
+    palq.sync()
+    done = first + live[-1] + 1 if live else top
+    pair.check(table, [done])
+    for t, was in zip((pair.gpu.k, pair.gpu.v, pair.gpu.k_scale, pair.gpu.v_scale), before):
+        assert torch.equal(t[[0, 2]], was[[0, 2]])
+        if not live:
+            assert torch.equal(t, was)
+    pair.fill(g, table, None)
+    k, v = torch.full((tokens, heads, dim), 5.0, device="cuda"), torch.full((tokens, heads, dim), 5.0, device="cuda")
+    palq.cache_read(pair.gpu, k, v, b)
+    palq.sync()
+    for out, which in ((k, "k"), (v, "v")):
+        want = np.full((tokens, heads, dim), 5.0, np.float32)
+        for h in range(heads):
+            vals = pair.ref.values(table, 0, top, h, which)[0]
+            for i in live:
+                want[i, h] = vals[first + i]
+        np.testing.assert_array_equal(host(out), want)
+    # attention: each row alone, as the last of a request that ends with it (the oracle's table without what is past `top`)
+    for causal, window in ((True, 0), (True, 4), (False, 0)):
+        q = dev(g.standard_normal((tokens, heads * 2, dim)), "f16")
+        out = torch.full_like(q, 3.0)
+        palq.attention(pair.gpu, q, out, b, 0.125, causal=causal, window=window)
+        palq.sync()
+        assert (host(out[n:]) == 3).all()
+        for i in range(n):
+            p = first + i
+            if causal and p < 0:
+                assert (host(out[i]) == 0).all()
+                continue
+            sees = [j for j in range(top) if not causal or (j <= p and (not window or j > p - window))]
+            if not sees:
+                assert (host(out[i]) == 0).all()
+                continue
+            # the same tokens, all seen by one row that ends with the last of them
+            span = sees[-1] + 1
+            check_attend(pair, host(out[i:i + 1]), table, [span], [0, 1], host(q[i:i + 1]), 0.125, "f16", causal=True,
+                         window=span - sees[0])
+
+
+@pytest.mark.parametrize("max_new,max_len", [(100, None), (None, 144), (90, 128)])
+def test_rows_left_out_of_tiles(palq, max_new, max_len):
+    """The same on the 128-row kernel: rows past max_new stay as they are, tokens past max_len are not seen, positions stay."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("left out of tiles", max_new, max_len)
+    g = np.random.default_rng(5)
+    page, dim, heads, lens, new = 16, 64, 16, [128, 150, 131, 260, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120]
+    table, pages = paged(g, lens, page)
+    pair = Pair(P, pages, heads, page, dim)
+    pair.fill(g, table, lens)
+    starts = cumsum(new)
+    q = dev(g.standard_normal((starts[-1], 2 * heads, dim)) * 1.5, "bf16")
+    b = pair.batch(table, lens, starts, max_new=max_new, max_len=max_len)
+    seen = table.copy()
+    if max_len:
+        seen[:, max_len // page:] = -1
+    for causal, window in ((True, 0), (True, 70), (False, 0)):
+        out = torch.full_like(q, 3.0)
+        palq.attention(pair.gpu, q, out, b, 0.125, causal=causal, window=window)
+        palq.sync()
+        got = host(out)
+        # the rows left out: replaced by what the oracle says, once they are seen to be as they were
+        left = np.zeros(starts[-1], bool)
+        for r, n in enumerate(new):
+            left[starts[r] + min(n, max_new or n):starts[r + 1]] = True
+        assert (got[left] == 3).all() and left.any() == bool(max_new)
+        got[left] = pair.ref.attend(seen, lens, starts, host(q), 0.125, causal, window)[0][left]
+        check_attend(pair, got, seen, lens, starts, host(q), 0.125, "bf16", causal=causal, window=window)
