@@ -66,7 +66,7 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Request &q,
   Reach s{0, q.len};
   if (a.causal) {
     s.hi = max(0, min(q.len, pos + 1));
-    if (a.window > 0) s.lo = max(0, pos - a.window + 1);
+    if (a.window > 0 && pos >= a.window) s.lo = pos - a.window + 1;  // (pos may be negative, the window near 2^31)
   }
   return s;
 }

@@ -168,3 +168,13 @@ def test_rows_left_out_of_tiles(palq, max_new, max_len):
         assert (got[left] == 3).all() and left.any() == bool(max_new)
         got[left] = pair.ref.attend(seen, lens, starts, host(q), 0.125, causal, window)[0][left]
         check_attend(pair, got, seen, lens, starts, host(q), 0.125, "bf16", causal=causal, window=window)
+
+
+@pytest.mark.parametrize("window", [1, 5, (1 << 31) - 1, (1 << 31) - 2, (1 << 31) - 40])
+def test_window_of_any_size_before_the_first_token(palq, window):
+    """More rows than tokens under a window: the rows before position 0 see nothing and take nothing from the others,
+    however large the window is (16, 32 and 128 rows a workgroup)."""
+    from paper_2208_01944_amd import palq as P
+    say("window", window)
+    for heads, group, lens, new in ((1, 1, [3, 30], [9, 5]), (2, 3, [10, 50], [33, 20]), (16, 4, [100, 30, 7, 60], [130, 100, 90, 60])):
+        attend_case(P, palq, heads, "bf16", 16, 64, heads, group, lens, new, True, window)
