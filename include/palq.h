@@ -511,7 +511,7 @@ typedef struct {
  *   max_new: at least every request's rows; max_len: at least every lens[r]
  *   (they size the launches; closer bounds run faster).
  * Device values outside these bounds never lead outside the tensors: rows
- * past max_new and tokens past max_len or the table are left out, as are
+ * past max_new and tokens past max_len, the table or 2^31 - 1024 are left out, as are
  * tokens on a page number outside [0, pages).  What is left out does not move
  * the rest: a row's position follows from lens and starts as they are. */
 typedef struct {

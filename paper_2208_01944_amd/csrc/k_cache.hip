@@ -63,14 +63,14 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView 
   const Request q = request_of(b, r, c.shift);
   const int old = max(0, q.pos);  // rows before position 0 have no place
   const int block = (old >> c.shift) + (int)blockIdx.x;
-  const int t0 = block << c.shift, lo = max(old, t0), hi = min(min(q.len, q.pos + q.n), t0 + c.page);
+  const int64_t t0 = (int64_t)block << c.shift, lo = max((int64_t)old, t0), hi = min((int64_t)min(q.len, q.pos + q.n), t0 + c.page);
   if (lo >= hi) return;
   const int pid = page_of(c, b, r, block);
   if (pid < 0) return;
-  const int kept = lo - t0, end = hi - t0, D = c.dim, groups = D / 8, items = append_items(c.page, D);
+  const int kept = (int)(lo - t0), end = (int)(hi - t0), D = c.dim, groups = D / 8, items = append_items(c.page, D);
   const R *src = (const R *)(values ? x.v : x.k);
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
-  src += (q.row0 + ((int64_t)t0 - q.pos)) * row + h * head;  // row of token t0 (there may be none)
+  src += (q.row0 + (t0 - q.pos)) * row + h * head;  // row of token t0 (there may be none)
   const int64_t ph = (int64_t)pid * c.heads + h;
   float *scale = (values ? c.vs : c.ks) + ph;
   const float had = kept ? *scale : 0.0f;
@@ -176,18 +176,19 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
   const Request q = request_of(b, r, c.shift);
   const int first = max(0, q.pos);
   const int block = (first >> c.shift) + (int)blockIdx.x;
-  const int t0 = block << c.shift, lo = max(first, t0), hi = min(min(q.len, q.pos + q.n), t0 + c.page);
+  const int64_t t0 = (int64_t)block << c.shift, lo = max((int64_t)first, t0), hi = min((int64_t)min(q.len, q.pos + q.n), t0 + c.page);
   if (lo >= hi) return;
+  const int from0 = (int)(lo - t0), end = (int)(hi - t0);  // the block's tokens that are read
   const int pid = page_of(c, b, r, block), D = c.dim;
   const int64_t ph = (int64_t)max(pid, 0) * c.heads + h;
   const float s = pid < 0 ? 0.0f : (values ? c.vs : c.ks)[ph];
   const int8_t *src = (values ? c.v : c.k) + ph * c.page * D;
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
-  R *dst = (R *)(values ? x.v : x.k) + (q.row0 + ((int64_t)lo - q.pos)) * row + h * head;
+  R *dst = (R *)(values ? x.v : x.k) + (q.row0 + (lo - q.pos)) * row + h * head;
   // several pieces' loads in flight before the first store
   if (!values) {
-    const int quads = D / 4, all = (hi - lo) * quads;
-    const uint32_t *from = (const uint32_t *)(src + (int64_t)(lo - t0) * D);
+    const int quads = D / 4, all = (end - from0) * quads;
+    const uint32_t *from = (const uint32_t *)(src + from0 * D);
     for (int p0 = threadIdx.x; p0 < all; p0 += 256 * 8) {
       uint32_t w[8];
 #pragma unroll
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
       }
     }
   } else {
-    const int c0 = (lo - t0) >> 4, all = (((hi - t0 + 15) >> 4) - c0) * D;
+    const int c0 = from0 >> 4, all = (((end + 15) >> 4) - c0) * D;
     for (int p0 = threadIdx.x; p0 < all; p0 += 256 * 2) {
       v4i o[2];
 #pragma unroll
@@ -217,8 +218,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
         if (p >= all) break;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const int t = t0 + at + j;
-          if (t >= lo && t < hi) dst[(int64_t)(t - lo) * row + d] = T::put((float)(int8_t)((uint32_t)o[i][j >> 2] >> (8 * (j & 3))) * s);
+          const int t = at + j;
+          if (t >= from0 && t < end) dst[(int64_t)(t - from0) * row + d] = T::put((float)(int8_t)((uint32_t)o[i][j >> 2] >> (8 * (j & 3))) * s);
         }
       }
     }

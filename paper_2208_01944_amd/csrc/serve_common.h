@@ -142,6 +142,7 @@ struct BatchView {
 // inside the tensors; what is left out (rows or tokens past the bounds) does not
 // move the others, so pos follows from lens and starts as they are.
 struct Request { int64_t row0; int32_t n, len, pos; };
+constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 1024;  // so that the tiles that are asked for past a request's end have 32-bit places
 __device__ __forceinline__ Request request_of(const BatchView &b, int r, int shift) {
   Request q;
   const int64_t s0 = b.starts[r], s1 = b.starts[r + 1], all = b.lens[r];
@@ -150,7 +151,7 @@ __device__ __forceinline__ Request request_of(const BatchView &b, int r, int shi
   const int64_t pos = all - (s1 - s0) + skip;
   q.pos = (int32_t)min(max(pos, (int64_t)-0x7fffffff), (int64_t)0x7fffffff);  // (no row reaches 0 from the one end, there are none at the other)
   q.n = (int32_t)max((int64_t)0, min(min(s1, b.tokens) - q.row0, b.max_new - skip));
-  q.len = (int32_t)max((int64_t)0, min(all, min((int64_t)b.max_pages << shift, b.max_len)));
+  q.len = (int32_t)max((int64_t)0, min(min(all, kMaxTokens), min((int64_t)b.max_pages << shift, b.max_len)));
   return q;
 }
 

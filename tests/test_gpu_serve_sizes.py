@@ -178,3 +178,45 @@ def test_window_of_any_size_before_the_first_token(palq, window):
     say("window", window)
     for heads, group, lens, new in ((1, 1, [3, 30], [9, 5]), (2, 3, [10, 50], [33, 20]), (16, 4, [100, 30, 7, 60], [130, 100, 90, 60])):
         attend_case(P, palq, heads, "bf16", 16, 64, heads, group, lens, new, True, window)
+
+
+@pytest.mark.parametrize("length", [(1 << 31) - 1024 - 5, (1 << 31) - 1024, (1 << 31) - 900, (1 << 31) - 1])
+@pytest.mark.parametrize("heads,group,new", [(2, 2, 3), (16, 4, 400)])
+def test_lengths_near_the_limit(palq, length, heads, group, new):
+    """Append, read and attention (rows and tiles) of the last positions next to 2^31 - 1024 tokens, and past it, where
+    tokens are left out: as the same rows and tokens 2^31 - 2048 places earlier."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("long", length, heads)
+    g = np.random.default_rng(3)
+    page, dim, room, base = 128, 64, 1 << 24, (1 << 31) - 2048
+    near = np.arange(1, 17, dtype=np.int32)[None]  # the pages of the last 2048 tokens
+    pair = Pair(P, 17, heads, page, dim)
+    pair.fill(g, near, None)
+    table = torch.zeros(1, room, dtype=torch.int32, device="cuda")
+    table[:, -16:] = dev(near)
+    starts, short, top = [0, new], length - base, 1024
+    b = P.Batch(table, dev(np.int32([length])), dev(np.int32(starts)), new, (1 << 31) - 1)
+    x, y = (g.standard_normal((new, heads, dim)).astype(np.float32) for _ in range(2))
+    left = max(0, min(top, short) - (short - new))  # rows with a place below the limit
+    if left:
+        pair.ref.append(near, [short - new + left], [0, left], x[:left], y[:left])
+    palq.cache_append(pair.gpu, dev(x), dev(y), b)
+    palq.sync()
+    pair.check(near, [min(top, short)])
+    k, v = torch.full((new, heads, dim), 5.0, device="cuda"), torch.full((new, heads, dim), 5.0, device="cuda")
+    palq.cache_read(pair.gpu, k, v, b)
+    palq.sync()
+    assert (host(k[left:]) == 5).all() and (host(v[left:]) == 5).all()
+    if left:
+        rk, rv = pair.ref.read(near, [short - new + left], [0, left])
+        np.testing.assert_array_equal(host(k[:left]), rk)
+        np.testing.assert_array_equal(host(v[:left]), rv)
+    seen = near.copy()
+    seen[:, top // page:] = -1
+    q = dev(g.standard_normal((new, heads * group, dim)), "bf16")
+    for window in (1, 300):
+        out = torch.full_like(q, 3.0)
+        palq.attention(pair.gpu, q, out, b, 0.125, window=window)
+        palq.sync()
+        check_attend(pair, host(out), seen, [short], starts, host(q), 0.125, "bf16", causal=True, window=window)
