@@ -548,8 +548,13 @@ palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_b
  * own position, with window > 0 only the last `window` of them; with
  * causal = 0 all (cross attention to cached encoder states: the rows then
  * have no position, and may outnumber the tokens).  A row that sees no token
- * gives 0; rows past max_new stay as they are.  Scores, softmax and sums are fp32; probabilities enter the second
- * product in fp16.  Long caches of few rows are split and joined in the
+ * gives 0; rows past max_new stay as they are.  Scores, softmax and sums are
+ * fp32; probabilities enter the second product in fp16: 11 bits, those below
+ * 2^-14 of the row's largest with an error of 2^-25 of it.  Scales are 0 or
+ * more, or NaN; blocks of any v_scale mix (0: the tokens count with the value
+ * 0), but one below 2^-20 of the largest among its 64 tokens (from a multiple
+ * of 64 on), or below 2^-72 of the largest of all, is rounded as if it had
+ * that scale.  Long caches of few rows are split and joined in the
  * context's workspace, which may grow (never while a graph is captured:
  * PALQ_ERR_NOMEM then; run the shape once before).  out and q (address ranges)
  * must not overlap. */

@@ -10,11 +10,19 @@
 // finished dot product.  Probabilities are rounded to fp16 (11 bits) as the
 // second product's operand.
 //
-// Value scales ride in the exponent: with u_j = log2(vs), w_j = exp2(s_j + u_j -
-// M), M the running maximum of s_j + u_j, the output is sum w_j code_j / L, L =
-// sum w_j / vs, so weights stay in fp16's range (at most 2^8: kSlack) whatever the
-// blocks' scales are, and no product with vs is left.  (Scales are at least 2^-100,
-// so 1 / vs and L stay finite.)
+// Value scales.  Blocks of any scale meet in one row, and a block whose scale one large
+// element sets may hold zeros in every other channel, so weights must keep their bits
+// beside a block of far larger scale.  vs = 2^(U + a) r: U, the unit that the
+// accumulators are in, follows the tiles' largest scales (within 4 powers of two of each
+// tile's, but at least 2^-72 of the largest so far: fp32 holds that); 2^a, -24 <= a <= 4,
+// goes into the fp16 codes, exactly, in the operation that converts them; what is left, r
+// in [1, 2), rides in the softmax's exponent: with u_j = log2 r, w_j = exp2(s_j + u_j - M),
+// M a running maximum, out = 2^U sum w_j (code_j 2^a) / L, L = sum w_j / r, and w stays
+// in fp16's range (at most 2^8 above the largest: kSlack).  Where a tile of 64 tokens has
+// one scale (prompts, pages of a tile or more), U lies 0 to 4 below it and r in [1, 32).
+// Blocks within 2^20 of their tile's largest scale, and tiles within 2^72 of all others,
+// lose nothing; below, r falls under 1, and fp16 has 11 bits of the weight for 14 powers
+// of two more.  A scale of 0 counts in L (r is held at 2^-64) and adds nothing else.
 //
 // Matrix layout.  S^T = K Q^T with v_mfma_f32_16x16x32_f16: a lane ends up with
 // scores of one query (lane % 16) and, row 4 c + i of subtile j standing for
@@ -45,6 +53,19 @@ __device__ __forceinline__ void codes_h4(uint32_t x, h2 &a, h2 &b) {
   a = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) - off;
   b = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) - off;
 }
+// The same times a power of two m (2^-24 to 2^4, or 0; n = -1152 m): as many operations.
+__device__ __forceinline__ void codes_h4(uint32_t x, h2 m, h2 n, h2 &a, h2 &b) {
+  const uint32_t u = x ^ 0x80808080u;
+  a = __builtin_elementwise_fma(__builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)), m, n);
+  b = __builtin_elementwise_fma(__builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)), m, n);
+}
+__device__ __forceinline__ h8 codes_h8(uint32_t x, uint32_t y, uint32_t mm, uint32_t nn) {
+  const h2 m = __builtin_bit_cast(h2, mm), n = __builtin_bit_cast(h2, nn);
+  h2 a, b, c, d;
+  codes_h4(x, m, n, a, b);
+  codes_h4(y, m, n, c, d);
+  return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
 __device__ __forceinline__ h8 codes_h8(uint32_t x, uint32_t y) {
   h2 a, b, c, d;
   codes_h4(x, a, b);
@@ -58,6 +79,40 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // up to 2^8 lose nothing in fp16 or fp32, and most tiles then leave the outputs'
 // accumulators alone.
 constexpr float kSlack = 8.0f;
+
+// The unit 2^u of the output accumulators (kNoUnit before the first scale).
+constexpr int kNoUnit = -512;
+__device__ __forceinline__ int exponent_of(float s) {  // of a normal number; kNoUnit of 0, inf and NaN
+  const int e = (int)(__float_as_uint(s) >> 23) & 255;
+  return e == 0 || e == 255 ? kNoUnit : e - 127;
+}
+struct Unit {
+  int u = kNoUnit, top = kNoUnit;
+  // e: the largest exponent of a tile's scales.  It stays within [u - BELOW, u + 4], and u within 72 of the
+  // largest e so far (2^72, weights of 2^13, codes of 2^7 and 2^31 tokens: sums stay in fp32).
+  template <int BELOW>
+  __device__ __forceinline__ bool leaves(int e) const { return e != kNoUnit && (e > u + 4 || e < u - BELOW); }
+  template <int BELOW>
+  __device__ __forceinline__ void follow(int e) {
+    top = max(top, e);
+    u = max(BELOW ? e : e - 2, top - 72);
+  }
+};
+// Scale over unit, q = vs / 2^U: its power of two 2^a goes into the codes (two halves of m, and of n = -1152 m), the
+// rest into the exponent (u, and 1 / r).
+struct ValueScale { float u, rv; uint32_t m, n; };
+__device__ __forceinline__ ValueScale value_scale(float q) {
+  const float p = fminf(fmaxf(__uint_as_float(__float_as_uint(q) & 0x7f800000u), 5.9604645e-8f), 16.0f);  // 2^-24 .. 2^4
+  const float r = q * __builtin_amdgcn_rcpf(p), l = __builtin_amdgcn_logf(r), u = l < -64.0f ? -64.0f : l;  // (NaN stays)
+  const float f = q == 0.0f ? 0.0f : p;
+  const h2 m = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(f, f)), n = m * h2{(_Float16)-1152.0f, (_Float16)-1152.0f};
+  return {u, exp2_fast(-u), __builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, n)};
+}
+// Where the whole tile has one scale, all of it goes into the exponent.
+__device__ __forceinline__ ValueScale value_scale_whole(float q) {
+  const float l = __builtin_amdgcn_logf(q), u = l < -64.0f ? -64.0f : l;
+  return {u, exp2_fast(-u), 0u, 0u};
+}
 
 // One row's reach: tokens [lo, hi).
 struct Reach { int lo, hi; };
@@ -115,6 +170,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
   constexpr int CH = D % 64 == 0 ? 16 : 8;  // consecutive channels of a key that a lane loads at once
   __shared__ float sm[4][NQ * 16], sl[4][NQ * 16];
+  __shared__ int su[4];
   __shared__ __attribute__((aligned(16))) float so[4][16 * OLD];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4;
   const int h = blockIdx.y, r = blockIdx.z, split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
@@ -151,6 +207,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   }
   v4f O[NQ][DT];
   float M[NQ], L[NQ];
+  Unit unit;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     M[n] = -INFINITY;
@@ -174,7 +231,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   auto load_k = [&](int tile) __attribute__((always_inline)) {
     const int kt = tile * 64 + kc, vt = tile * 64 + vc;
     const bool kok = ((uint32_t)kpage < (uint32_t)cv.pages) & (kt < hi);
-    vthere = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
+    vthere = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi) & (vt + 16 > lo);
     const int8_t *kb = cv.k + (((int64_t)(kok ? kpage : 0) * heads + h) * cv.page + (kt & pm) + (col & 3)) * D + c * CH;
     const int64_t sc = (int64_t)(vthere ? vpage : 0) * heads + h;
     ks = cv.ks[sc];
@@ -234,6 +291,22 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     const int vt = tile * 64 + vc;
     const bool there = vthere;
     const float kst = ks, vst = vs;
+    // (no scale of the tile from 2^5 on, one from 2^-4 on: the unit stays)
+    float vq = __builtin_ldexpf(vst, -unit.u);
+    if (__any(there & (vq >= 32.0f)) || !__any(there & (vq >= 0.0625f))) {
+      const int ve = there ? exponent_of(vst) : kNoUnit, was = unit.u;
+      const int most = max(max(__builtin_amdgcn_readlane(ve, 0), __builtin_amdgcn_readlane(ve, 16)),
+                           max(__builtin_amdgcn_readlane(ve, 32), __builtin_amdgcn_readlane(ve, 48)));
+      if (unit.leaves<4>(most)) unit.follow<4>(most);
+      const float by = __builtin_ldexpf(1.0f, was - unit.u);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) O[n][d] *= by;
+      vq = __builtin_ldexpf(vst, -unit.u);
+    }
+    const ValueScale vsc = value_scale(vq);
+    const float u = vsc.u, rv = vsc.rv;
     v4f S[NQ][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -248,7 +321,6 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
         for (int n = 0; n < NQ; ++n) S[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, Q[n][s], S[n][j], 0, 0, 0);
       }
     if constexpr (more) load_k(tile + 4);
-    const float u = __builtin_amdgcn_logf(vst), rv = __builtin_amdgcn_rcpf(vst);
     h8 P[NQ][2];
     // Tokens that all rows see need no masks (columns past the last row are not stored).
     // 8 requests of 17 to 131 rows, heads of 64: 17.7 us, 19.9 with masks always.  The wider
@@ -303,7 +375,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const h8 A = codes_h8((uint32_t)vx[d][2 * s], (uint32_t)vx[d][2 * s + 1]);
+        const h8 A = codes_h8((uint32_t)vx[d][2 * s], (uint32_t)vx[d][2 * s + 1], vsc.m, vsc.n);
 #pragma unroll
         for (int n = 0; n < NQ; ++n) O[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, P[n][s], O[n][d], 0, 0, 0);
       }
@@ -314,7 +386,8 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   for (; tile + 4 < te; tile += 4) step(tile, std::false_type());
   if (tile < te) step(tile, std::true_type());
 
-  // the waves' results under one maximum
+  // the waves' results under one maximum and in one unit
+  if (lane == 0) su[wave] = unit.u;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     float l = L[n];
@@ -326,11 +399,12 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     }
   }
   __syncthreads();
+  const int ut = max(max(su[0], su[1]), max(su[2], su[3]));
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int rc = n * 16 + col;
     const float mt = fmaxf(fmaxf(sm[0][rc], sm[1][rc]), fmaxf(sm[2][rc], sm[3][rc]));
-    const float wgt = exp2_fast(M[n] - (mt == -INFINITY ? 0.0f : mt));
+    const float wgt = __builtin_ldexpf(exp2_fast(M[n] - (mt == -INFINITY ? 0.0f : mt)), unit.u - ut);
 #pragma unroll
     for (int d = 0; d < DT; ++d) *(v4f *)&so[wave][col * OLD + d * 16 + c * 4] = O[n][d] * wgt;
     __syncthreads();
@@ -349,18 +423,15 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
       for (int w = 0; w < 4; ++w) l += sl[w][rq] * exp2_fast(sm[w][rq] - (m == -INFINITY ? 0.0f : m));
       if (a.splits == 1) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        const float v[4] = {__builtin_ldexpf(o[0] * inv, ut), __builtin_ldexpf(o[1] * inv, ut), __builtin_ldexpf(o[2] * inv, ut),
+                            __builtin_ldexpf(o[3] * inv, ut)};
         uint16_t *dst = a.out + (q.row0 + t) * a.out_row + (int64_t)hq * a.out_head + d;
         store4<T>(dst, v);
       } else {
         const int64_t hs = (int64_t)cv.heads * a.group;
         const int64_t at = ((int64_t)split * a.b.tokens + q.row0 + t) * hs + hq;
         *(v4f *)(a.part + at * D + d) = o;
-        if (d == 0) {
-          float *ml = a.part + (int64_t)a.splits * a.b.tokens * hs * D + at * 2;
-          ml[0] = m;
-          ml[1] = l;
-        }
+        if (d == 0) *(v4f *)(a.part + (int64_t)a.splits * a.b.tokens * hs * D + at * 4) = v4f{m, l, (float)ut, 0.0f};
       }
     }
     __syncthreads();
@@ -415,7 +486,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   typedef TileLds<D> G;
   constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + kTileThreads - 1) / kTileThreads;
   __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
-  __shared__ float4 blocks[4][4];  // of four tiles' 16-token chunks: {ks, log2 vs, 1 / vs, page there}
+  __shared__ float4 blocks[4][4];  // of four tiles' 16-token chunks: {ks, u, 1 / r, page there}
+  __shared__ uint2 factors[4][4];  // narrow pages: and the factor of their values' codes (m, n)
+  __shared__ int units[4];         // and the tiles' units
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, c = lane >> 5;
   // cache heads go fastest, so a head's tiles share one XCD's L2 where heads are a
   // multiple of 8; the rows with the longest reach start first
@@ -520,19 +593,41 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       kx[i] = *(const v4i *)(kh + kp + tile_key_at(pc, ktile, pm, D));
       vx[i] = *(const v4i *)(vh + vp + tile_value_at(pc, vtile, pm, cv.shift));
     }
-    const bool page = valid(e.b);
+    const bool page = valid(e.b), reached = p * 64 + (int)(threadIdx.x & 3) * 16 + 16 > rf.lo;  // (what no row sees sets no unit)
     const int64_t at = (int64_t)(page ? e.b : 0) * heads + h;
     bks = cv.ks[at];
     bvs = cv.vs[at];
-    bthere = page ? 1.0f : 0.0f;
+    bthere = page && reached ? 1.0f : 0.0f;
   };
   // keys of tile p and values of tile p - 1 to their places, then the loads of the
   // next.  Loads end in order, so the entries that the next call needs come first.
   // None of it stands under a condition, so that waits count only what they need; past
   // the last tile it reads tiles that nobody uses.  par: p - tb is odd.
-  auto bring_blocks = [&](int p) __attribute__((always_inline)) {
-    if (wave == 0 && lane < 4)
-      blocks[(p - tb) & 3][lane] = make_float4(bks, __builtin_amdgcn_logf(bvs), __builtin_amdgcn_rcpf(bvs), bthere);
+  // WIDE: one scale a tile, which every wave follows in scalar registers (the units of two
+  // tiles, by their parity); else wave 0 follows the largest, and the others read LDS.
+  Unit unit;
+  int wide_unit[2] = {kNoUnit, kNoUnit};
+  auto bring_blocks = [&](int p, auto par) __attribute__((always_inline)) {
+    if constexpr (WIDE) {
+      const int e = valid(ent[decltype(par)::value].b) ? exponent_of(bvs) : kNoUnit;
+      if (unit.leaves<0>(e)) unit.follow<0>(e);
+      wide_unit[decltype(par)::value] = unit.u;
+      if (wave == 0 && lane < 4) {
+        const ValueScale v = value_scale_whole(__builtin_ldexpf(bvs, -unit.u));
+        blocks[(p - tb) & 3][lane] = make_float4(bks, v.u, v.rv, bthere);
+      }
+    } else if (wave == 0) {
+      const int e = bthere != 0.0f ? exponent_of(bvs) : kNoUnit;
+      const int most = max(max(__builtin_amdgcn_readlane(e, 0), __builtin_amdgcn_readlane(e, 1)),
+                           max(__builtin_amdgcn_readlane(e, 2), __builtin_amdgcn_readlane(e, 3)));
+      if (unit.leaves<4>(most)) unit.follow<4>(most);
+      const ValueScale v = value_scale(__builtin_ldexpf(bvs, -unit.u));
+      if (lane < 4) {
+        blocks[(p - tb) & 3][lane] = make_float4(bks, v.u, v.rv, bthere);
+        factors[(p - tb) & 3][lane] = make_uint2(v.m, v.n);
+      }
+      if (lane == 0) units[(p - tb) & 3] = unit.u;
+    }
   };
   auto bring = [&](int p, auto par) __attribute__((always_inline)) {
     constexpr int odd = decltype(par)::value;
@@ -547,8 +642,14 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       *(h8 *)(kd + 512) = codes_h8((uint32_t)kx[i][2], (uint32_t)kx[i][3]);
       // operand (32 channels, subtile, k): lane 32 c + channel has 8 tokens from 16 c + 8 k
       uint8_t *vd = vbase + (pc.d >> 5) * 4096 + (pc.vt >> 5) * 2048 + (pc.vt >> 4 & 1) * 512 + (pc.d & 31) * 16;
-      *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1]);
-      *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3]);
+      if constexpr (WIDE) {
+        *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1]);
+        *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3]);
+      } else {
+        const uint2 f = factors[(p - 1 - tb) & 3][pc.vt >> 4];  // (of tile p - 1, in LDS since the last step)
+        *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1], f.x, f.y);
+        *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3], f.x, f.y);
+      }
     }
     entries(p + 2, ent[odd]);
     load(p + 1, ent[odd ^ 1]);
@@ -560,6 +661,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
 #pragma unroll
     for (int i = 0; i < 16; ++i) O[d][i] = 0.0f;
   float M = -INFINITY, L = 0.0f;
+  int ou = kNoUnit;  // the unit of O
   v16f S[2];
   h8 P[2][2];
   bool busy = false;  // this wave has scores, or weights, of the present tile
@@ -594,7 +696,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     constexpr std::integral_constant<int, decltype(which)::value ^ 1> other;
     const bool next = i < te && i * 64 < any_hi && i * 64 + 64 > any_lo;
     if (i < te) {
-      bring_blocks(i + 1);
+      bring_blocks(i + 1, other);
       bring(i + 1, other);
     }
     if (busy) second(which);
@@ -607,6 +709,13 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     if (!busy) return;
     const int t0 = i * 64;
     const float4 b0 = blocks[(i - tb) & 3][c], b1 = blocks[(i - tb) & 3][2 + c];
+    const int tu = WIDE ? wide_unit[b] : __builtin_amdgcn_readfirstlane(units[(i - tb) & 3]), moved = ou - tu;
+    ou = tu;
+    if (moved) {
+      const float by = __builtin_ldexpf(1.0f, moved);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) O[d] *= by;
+    }
     // tokens of this lane that its row does not see, where there are any
     const bool masked = !(__all(b0.w != 0.0f && b1.w != 0.0f) && t0 >= all_lo && t0 + 64 <= all_hi);
     uint32_t off = 0;
@@ -623,7 +732,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
         }
       }
     }
-    // s fk + lv, fk >= 0: the largest comes from the largest product
+    // s fk, fk >= 0: the largest comes from the largest product (of the scores alone: a wide tile's lv is up to 5)
     const float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
     float mx = -INFINITY;
 #pragma unroll
@@ -631,7 +740,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       float m = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 16; ++j) m = fmaxf(m, S[u][j]);
-      mx = fmaxf(mx, m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[u], lv[u]));
+      mx = fmaxf(mx, m == -INFINITY ? -INFINITY : m * fk[u]);
     }
     mx = other_half_max(mx);
     if (__any(mx > M + kSlack)) {
@@ -667,7 +776,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     entries(tb, ent[0]);
     entries(tb + 1, ent[1]);
     load(tb, ent[0]);
-    bring_blocks(tb);
+    bring_blocks(tb, even);
     bring(tb, even);  // (there are no values yet: those of tile tb, twice)
     __syncthreads();
     // One barrier a step: what a step brings to LDS is read in the next, and takes the
@@ -696,11 +805,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *(v4f *)(dst + d * 32 + g * 8 + c * 4) = v4f{O[d][4 * g], O[d][4 * g + 1], O[d][4 * g + 2], O[d][4 * g + 3]};
-    if (c == 0) {
-      float *ml = a.part + (int64_t)a.splits * a.b.tokens * hs * D + at * 2;
-      ml[0] = M;
-      ml[1] = L;
-    }
+    if (c == 0) *(v4f *)(a.part + (int64_t)a.splits * a.b.tokens * hs * D + at * 4) = v4f{M, L, (float)ou, 0.0f};
     return;
   }
   // rows through LDS (the last barrier came after every wave's last read), a wave's own part
@@ -711,7 +816,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const float v[4] = {O[d][4 * g] * inv, O[d][4 * g + 1] * inv, O[d][4 * g + 2] * inv, O[d][4 * g + 3] * inv};
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __builtin_ldexpf(O[d][4 * g + i] * inv, ou);
       store4<T>(my + col * LD + d * 32 + g * 8 + c * 4, v);
     }
   __builtin_amdgcn_wave_barrier();
@@ -726,7 +833,8 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   }
 }
 
-// One (token, head) row a group of D / 4 threads: the splits under one maximum.
+// One (token, head) row a group of D / 4 threads: the splits under one maximum and
+// in one unit.
 template <class T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int W = D / 4;
@@ -738,33 +846,39 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   const int64_t t = i / hs, hq = i - t * hs, at = (q.row0 + t) * hs + hq, step = a.b.tokens * hs;
   const float *ml = a.part + a.splits * step * D;
   // eight splits at a time, all their loads in flight
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l = 0.0f, u = kNoUnit;
   v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int s0 = 0; s0 < a.splits; s0 += 8) {
-    v2f x[8];
+    v4f x[8];
     v4f y[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       const int64_t from = min(s0 + s, a.splits - 1) * step + at;
-      x[s] = *(const v2f *)(ml + from * 2);
+      x[s] = *(const v4f *)(ml + from * 4);
       y[s] = *(const v4f *)(a.part + from * D + d);
     }
-    float mn = m;
+    float mn = m, un = u;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) mn = fmaxf(mn, x[s][0]);
+    for (int s = 0; s < 8; ++s) {
+      mn = fmaxf(mn, x[s][0]);
+      un = fmaxf(un, x[s][2]);
+    }
     const float ms = mn == -INFINITY ? 0.0f : mn, w0 = exp2_fast(m - ms);
-    m = mn;
     l *= w0;
-    o *= w0;
+    o *= __builtin_ldexpf(w0, (int)(u - un));
+    m = mn;
+    u = un;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       const float w = s0 + s < a.splits ? exp2_fast(x[s][0] - ms) : 0.0f;
       l += x[s][1] * w;
-      o += y[s] * w;
+      o += y[s] * __builtin_ldexpf(w, (int)(x[s][2] - u));
     }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const float v[4] = {o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+  float v[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = __builtin_ldexpf(o[k] * inv, (int)u);
   uint16_t *dst = a.out + (q.row0 + t) * a.out_row + hq * a.out_head + d;
   store4<T>(dst, v);
 }
@@ -825,7 +939,7 @@ bool attend_plan(AttendArgs &a, int cus) {
 
 size_t attend_work_bytes(const AttendArgs &a) {
   if (a.splits == 1) return 0;
-  return (size_t)a.splits * a.b.tokens * a.c.heads * a.group * (a.c.dim + 2) * sizeof(float);
+  return (size_t)a.splits * a.b.tokens * a.c.heads * a.group * (a.c.dim + 4) * sizeof(float);
 }
 
 hipError_t launch_attend(const AttendArgs &a, int type, hipStream_t s) {
