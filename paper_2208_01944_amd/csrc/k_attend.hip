@@ -5,10 +5,10 @@
 //
 // Scores and sums are fp32.  The codes are exact in fp16, so q is the only
 // operand that is rounded: each row is scaled by a power of two that brings its
-// largest element to [1, 2) (bf16 values, 8 bits, stay exact but for elements
-// 2^-15 below the row's largest), and the scale of a block multiplies the
-// finished dot product.  Probabilities are rounded to fp16 (11 bits) as the
-// second product's operand.
+// largest element to [2^14, 2^15), the top of fp16's range, so that bf16 values (8 bits)
+// stay exact down to 2^-31 of the row's largest and fp16 values (11 bits) down to 2^-28;
+// the scale of a block multiplies the finished dot product.  Probabilities are rounded to
+// fp16 (11 bits) as the second product's operand.
 //
 // Value scales.  Blocks of any scale meet in one row, and a block whose scale one large
 // element sets may hold zeros in every other channel, so weights must keep their bits
@@ -126,13 +126,13 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Request &q,
   return s;
 }
 
-// The power of two that brings a row's largest magnitude (its bits) to [1, 2),
+// The power of two that brings a row's largest magnitude (its bits) to [2^14, 2^15),
 // and its inverse.  A row with inf or NaN: 0, so that inf 0 = NaN reaches all of
 // its scores.
 struct RowScale { float in, out; };
 __device__ __forceinline__ RowScale row_scale(uint32_t mag) {
-  const int e = (int)(mag >> 23), b = min(max(e, 1), 253);
-  return {e == 255 ? 0.0f : __uint_as_float((uint32_t)(254 - b) << 23), __uint_as_float((uint32_t)b << 23)};
+  const int e = (int)(mag >> 23), b = min(max(e, 15), 254);
+  return {e == 255 ? 0.0f : __uint_as_float((uint32_t)(268 - b) << 23), __uint_as_float((uint32_t)(b - 14) << 23)};
 }
 
 template <class T>

@@ -133,3 +133,25 @@ def test_attention_scales_of_any_size(palq, shape, page, dim, spread):
     with np.errstate(invalid="ignore"):
         out = attend(palq, pair, table, lens, starts, q, b)
     assert np.isnan(out).any()
+
+
+@pytest.mark.parametrize("power", [10, 20, 26])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape,page,dim", [("rows16", 16, 64), ("rows32", 64, 96), ("splits", 32, 128), ("rows16", 64, 256), ("tiles", 16, 64)])
+def test_attention_one_large_query_element(palq, shape, page, dim, dtype, power):
+    """One element of a query 2^power times the others, in a channel in which the keys are 0: scores come from the others."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("one large query element", shape, page, dim, dtype, power)
+    g, pair, table, lens, starts, q, b = case(P, shape, page, dim, 4)
+    pair.fill(g, table, lens)
+    pair.ref.k[..., 5] = 0
+    pair.upload()
+    x = g.standard_normal(tuple(q.shape)) * 2.0 ** (-13 if dtype == "f16" else 0)
+    x[..., 5] = 2.0 ** (power - (13 if dtype == "f16" else 0)) * 1.5
+    q = dev(x, dtype)
+    out = torch.full_like(q, 3.0)
+    scale = 0.125 * 2.0 ** (13 if dtype == "f16" else 0)
+    palq.attention(pair.gpu, q, out, b, scale)
+    palq.sync()
+    check_channels(pair, host(out), table, lens, starts, host(q), scale, dtype)
