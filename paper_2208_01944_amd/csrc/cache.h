@@ -20,7 +20,7 @@ struct AttendArgs {
   int64_t q_row, q_head, out_row, out_head;  // strides in elements
   int32_t group;                             // query heads of a cache head
   int32_t causal, window;
-  float scale;                               // of the scores, times log2(e)
+  float scale;                               // of the scores
   int32_t block;                             // rows of a workgroup
   int32_t splits;                            // parts that a request's tokens are cut into
   float *part;                               // their results (attend_work_bytes)

@@ -75,6 +75,8 @@ __device__ __forceinline__ h8 codes_h8(uint32_t x, uint32_t y) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+constexpr float kLog2e = 1.44269504088896340736f;  // (times the row's factor first: scales near 2^128 are numbers too)
+
 // The running maximum moves only when a score passes it by more than 2^8: weights
 // up to 2^8 lose nothing in fp16 or fp32, and most tiles then leave the outputs'
 // accumulators alone.
@@ -284,7 +286,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     if (a.scale < 0.0f) rs.in = -rs.in;  // the factor of the products stays >= 0
 #pragma unroll
     for (int s = 0; s < KS; ++s) Q[n][s] = scaled<T>(raw[n][s], rs.in);
-    f[n] = rs.out * fabsf(a.scale);
+    f[n] = rs.out * kLog2e * fabsf(a.scale);
   }
   auto step = [&](int tile, auto last) __attribute__((always_inline)) {
     constexpr bool more = !decltype(last)::value;
@@ -530,7 +532,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     if (a.scale < 0.0f) rs.in = -rs.in;  // the factor of the products stays >= 0
 #pragma unroll
     for (int s = 0; s < KS; ++s) Q[s] = scaled<T>(raw[s], rs.in);
-    f = rs.out * fabsf(a.scale);
+    f = rs.out * kLog2e * fabsf(a.scale);
   }
 
   const int32_t *table = a.b.table + (int64_t)r * a.b.max_pages;

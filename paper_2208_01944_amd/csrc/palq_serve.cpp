@@ -320,7 +320,7 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
   if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0) return PALQ_OK;
   hipSetDevice(ctx->device);
   AttendArgs a{view_of(cache), view_of(batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
-               group, causal, window, scale * 1.44269504088896340736f, 0, 1, nullptr};
+               group, causal, window, scale, 0, 1, nullptr};
   if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
   if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^31 or more workgroups");
   if (const size_t need = attend_work_bytes(a)) {

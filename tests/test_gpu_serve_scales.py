@@ -155,3 +155,21 @@ def test_attention_one_large_query_element(palq, shape, page, dim, dtype, power)
     palq.attention(pair.gpu, q, out, b, scale)
     palq.sync()
     check_channels(pair, host(out), table, lens, starts, host(q), scale, dtype)
+
+
+@pytest.mark.parametrize("shape", ["rows16", "rows32", "splits", "tiles"])
+@pytest.mark.parametrize("scale", [1.75 * 2.0 ** 127, -1.75 * 2.0 ** 127, 2.0 ** -120])
+def test_attention_scales_of_the_scores_near_the_ends(palq, shape, scale):
+    """Finite scales whose product with log2(e) is none, and tiny ones, with queries and keys that bring the scores back."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("score scale", shape, scale)
+    g, pair, table, lens, starts, q, b = case(P, shape, 16, 64, 6)
+    pair.fill(g, table, lens)
+    q = dev(g.standard_normal(tuple(q.shape)) * (2.0 ** -100 if abs(scale) > 1 else 2.0 ** 90), "bf16")
+    pair.ref.ks[:] *= np.float32(2.0 ** -30 if abs(scale) > 1 else 2.0 ** 27)
+    pair.upload()
+    out = torch.full_like(q, 3.0)
+    palq.attention(pair.gpu, q, out, b, scale)
+    palq.sync()
+    check_channels(pair, host(out), table, lens, starts, host(q), scale, "bf16")
