@@ -535,7 +535,9 @@ palq_status palq_cache_append(palq_ctx *ctx, const palq_cache *cache, const palq
 /* The inverse: code * scale of each request's last tokens, to tensors laid
  * out as in palq_cache_append; 0 for tokens on pages out of range.  Rows that
  * are left out, or whose position is none of the request's (before 0, or past
- * max_len or the table), stay as they are. */
+ * max_len or the table), stay as they are.  Tensors that a call writes have no
+ * two rows over each other and none over the cache; k and v may be parts of
+ * one fused tensor. */
 palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, void *k, int64_t k_row,
                             int64_t k_head, void *v, int64_t v_row, int64_t v_head, int32_t type);
 

@@ -124,6 +124,37 @@ palq_status check_rows(palq_ctx *ctx, const void *p, int64_t tokens, int64_t row
   return PALQ_OK;
 }
 
+// Whether any row (dim elements) of a tensor of rows t, heads h at t row + h head lies over another of its own, or,
+// with `apart` elements between them, over one of a second tensor of the same strides.
+bool rows_meet(int64_t tokens, int64_t row, int32_t heads, int64_t head, int32_t dim, int64_t apart, bool own) {
+  const int64_t cols = (heads - 1) * head + dim, all = (tokens - 1) * row + cols, gap = apart < 0 ? -apart : apart;
+  if (own ? row >= cols || head >= (tokens - 1) * row + dim : gap >= all || (gap >= cols && row >= gap + cols)) return false;
+  for (int64_t h = own ? 0 : 1 - heads; h < heads; ++h) {
+    // t row + h head + apart within (-dim, dim) for a t of (-tokens, tokens)
+    const int64_t off = h * head + apart;
+    if (tokens == 1 || row == 0) {
+      if (off > -dim && off < dim && !(own && h == 0)) return true;
+      continue;
+    }
+    for (int64_t t = -off / row - 1; t <= -off / row + 1; ++t)
+      if (t > -tokens && t < tokens && !(own && h == 0 && t == 0) && t * row + off > -dim && t * row + off < dim) return true;
+  }
+  return false;
+}
+
+// Tensors that a call writes: no two rows over each other, none over the cache.
+palq_status check_written(palq_ctx *ctx, const palq_cache *c, const void *p, int64_t tokens, int64_t row, int64_t head,
+                          int32_t heads, int32_t type) {
+  if (tokens <= 0) return PALQ_OK;
+  if (rows_meet(tokens, row, heads, head, c->head_dim, 0, true)) return fail(ctx, PALQ_ERR_ARG, "output: rows overlap");
+  const int64_t bytes = ((tokens - 1) * row + (heads - 1) * head + c->head_dim) * size_of(type);
+  const int64_t blocks = (int64_t)c->pages * c->heads, codes = blocks * c->page_tokens * c->head_dim;
+  if (overlaps(p, bytes, c->k, codes) || overlaps(p, bytes, c->v, codes) || overlaps(p, bytes, c->k_scale, blocks * 4) ||
+      overlaps(p, bytes, c->v_scale, blocks * 4))
+    return fail(ctx, PALQ_ERR_ARG, "output: overlaps the cache");
+  return PALQ_OK;
+}
+
 CacheView view_of(const palq_cache *c) {
   CacheView v{c->k, c->v, c->k_scale, c->v_scale, c->pages, c->heads, c->head_dim, c->page_tokens, 0};
   while ((1 << v.shift) < v.page) ++v.shift;
@@ -287,6 +318,16 @@ palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_b
   if ((st = check_rows(ctx, k, batch->tokens, k_row, k_head, cache->heads, cache->head_dim, type)) ||
       (st = check_rows(ctx, v, batch->tokens, v_row, v_head, cache->heads, cache->head_dim, type)))
     return st;
+  if ((st = check_written(ctx, cache, k, batch->tokens, k_row, k_head, cache->heads, type)) ||
+      (st = check_written(ctx, cache, v, batch->tokens, v_row, v_head, cache->heads, type)))
+    return st;
+  if (batch->tokens > 0) {  // (k and v may share rows of a fused tensor, but no element)
+    const int64_t apart = (const char *)v - (const char *)k, size = size_of(type);
+    const bool alike = k_row == v_row && k_head == v_head;
+    if (alike ? rows_meet(batch->tokens, k_row, cache->heads, k_head, cache->head_dim, apart / size, false)
+              : apart > -cache->head_dim * size && apart < cache->head_dim * size)
+      return fail(ctx, PALQ_ERR_ARG, "cache read: k and v overlap");
+  }
   if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0 || batch->max_len == 0)
     return PALQ_OK;
   hipSetDevice(ctx->device);
@@ -317,6 +358,7 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
   };
   if (overlaps(q, bytes(q_row, q_head), out, bytes(out_row, out_head)))
     return fail(ctx, PALQ_ERR_ARG, "attention: out overlaps q");
+  if ((st = check_written(ctx, cache, out, batch->tokens, out_row, out_head, q_heads, type))) return st;
   if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0) return PALQ_OK;
   hipSetDevice(ctx->device);
   AttendArgs a{view_of(cache), view_of(batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
