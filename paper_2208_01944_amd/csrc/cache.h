@@ -26,7 +26,7 @@ struct AttendArgs {
   float *part;                               // their results (attend_work_bytes)
 };
 
-// Chooses kernel and parts (false: a grid past 2^31), and the device memory for the parts.
+// Chooses kernel and parts (false: a row tile of all requests is no launch), and the device memory for the parts.
 bool attend_plan(AttendArgs &a, int cus);
 size_t attend_work_bytes(const AttendArgs &a);
 hipError_t launch_attend(const AttendArgs &a, int type, hipStream_t s);

@@ -484,7 +484,7 @@ __device__ __forceinline__ void ahead() {
 }
 
 template <class T, int D, bool WIDE>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int row_tiles) {
+__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int first_tile, int row_tiles) {
   typedef TileLds<D> G;
   constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + kTileThreads - 1) / kTileThreads;
   __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
@@ -496,7 +496,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   // multiple of 8; the rows with the longest reach start first
   const int heads = a.c.heads, combos = heads * a.b.requests;
   const int combo = blockIdx.x % combos, rest = blockIdx.x / combos;
-  const int h = combo % heads, r = (combo / heads + rest) % a.b.requests, split = rest % a.splits, rt = row_tiles - 1 - rest / a.splits;
+  const int h = combo % heads, r = (combo / heads + rest) % a.b.requests, split = rest % a.splits, rt = first_tile + row_tiles - 1 - rest / a.splits;
   const CacheView &cv = a.c;
   const Request q = request_of(a.b, r, cv.shift);
   const int rows = q.n * a.group, first = rt * ROWS;
@@ -899,9 +899,14 @@ template <class T, int D>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
   if (a.block == 128) {
-    const unsigned flat = (unsigned)(rt * a.splits * a.c.heads * a.b.requests);
-    if (a.c.page >= 64) attend_tile_kernel<T, D, true><<<flat, 256, 0, s>>>(a, (int)rt);
-    else attend_tile_kernel<T, D, false><<<flat, 256, 0, s>>>(a, (int)rt);
+    // one launch, unless loose bounds make it too large: then the last rows' first
+    const int64_t each = (int64_t)a.splits * a.c.heads * a.b.requests, most = kMaxGroups / each;
+    for (int64_t left = rt; left > 0; left -= most) {
+      const int64_t n = std::min(left, most), t0 = left - n;
+      const unsigned flat = (unsigned)(n * each);
+      if (a.c.page >= 64) attend_tile_kernel<T, D, true><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
+      else attend_tile_kernel<T, D, false><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
+    }
   } else {
     const dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
     if (a.block == 16) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
@@ -936,7 +941,7 @@ bool attend_plan(AttendArgs &a, int cus) {
   // done in four is not cut at all: joining costs as much.
   const int64_t most = a.b.max_len <= 1024 ? 1 : (a.b.max_len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), want / base));
-  return base * a.splits < (int64_t)1 << 31;
+  return (int64_t)a.splits * a.c.heads * a.b.requests <= kMaxGroups;
 }
 
 size_t attend_work_bytes(const AttendArgs &a) {

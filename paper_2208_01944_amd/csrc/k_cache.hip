@@ -54,7 +54,7 @@ struct NewKv {
 // NI items a thread hold a whole block in registers, so new values are read once.
 // Values are turned (a word of 4 tokens for each channel) through LDS.
 template <class T, int NI>
-__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView c, BatchView b, NewKv x) {
+__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView c, BatchView b, NewKv x, int block0) {
   typedef typename T::raw R;
   __shared__ uint32_t part[4];
   __shared__ uint32_t turned[turned_words(NI)];  // [dim][turned_stride]
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView 
   const bool values = blockIdx.z & 1;
   const Request q = request_of(b, r, c.shift);
   const int old = max(0, q.pos);  // rows before position 0 have no place
-  const int block = (old >> c.shift) + (int)blockIdx.x;
+  const int block = (old >> c.shift) + block0 + (int)blockIdx.x;
   const int64_t t0 = (int64_t)block << c.shift, lo = max((int64_t)old, t0), hi = min((int64_t)min(q.len, q.pos + q.n), t0 + c.page);
   if (lo >= hi) return;
   const int pid = page_of(c, b, r, block);
@@ -169,13 +169,13 @@ struct OutKv {
 };
 
 template <class T>
-__global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView b, OutKv x) {
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView b, OutKv x, int block0) {
   typedef typename T::raw R;
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
   const Request q = request_of(b, r, c.shift);
   const int first = max(0, q.pos);
-  const int block = (first >> c.shift) + (int)blockIdx.x;
+  const int block = (first >> c.shift) + block0 + (int)blockIdx.x;
   const int64_t t0 = (int64_t)block << c.shift, lo = max((int64_t)first, t0), hi = min((int64_t)min(q.len, q.pos + q.n), t0 + c.page);
   if (lo >= hi) return;
   const int from0 = (int)(lo - t0), end = (int)(hi - t0);  // the block's tokens that are read
@@ -227,38 +227,51 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
 }
 
 // Blocks that max_new tokens behind any number of old ones can touch.
-unsigned blocks_of(const CacheView &c, const BatchView &b) {
-  const int64_t n = std::min<int64_t>(b.max_new, b.max_len);
-  return (unsigned)std::min<int64_t>((n + c.page - 2) / c.page + 1, b.max_pages);
+int64_t blocks_of(const CacheView &c, const BatchView &b) {
+  const int64_t n = std::min(std::min<int64_t>(b.max_new, b.max_len), b.tokens);
+  return std::min<int64_t>((n + c.page - 2) / c.page + 1, b.max_pages);
+}
+
+// Launches f(grid, first block) over all blocks of a batch.
+template <class F>
+void over_blocks(const CacheView &c, const BatchView &b, F f) {
+  const int64_t blocks = blocks_of(c, b);
+  for (int64_t b0 = 0; b0 < blocks; b0 += kMaxGroups)
+    f(dim3((unsigned)std::min(blocks - b0, kMaxGroups), (unsigned)c.heads, (unsigned)b.requests * 2), (int)b0);
 }
 
 template <class T>
-void launch_append_t(dim3 g, const CacheView &c, const BatchView &b, const NewKv &x, hipStream_t s) {
+void launch_append_t(const CacheView &c, const BatchView &b, const NewKv &x, hipStream_t s) {
   const int n = append_rounds(c.page, c.dim);
-  if (n == 1) cache_append_kernel<T, 1><<<g, kAppendThreads, 0, s>>>(c, b, x);
-  else if (n == 2) cache_append_kernel<T, 2><<<g, kAppendThreads, 0, s>>>(c, b, x);
-  else cache_append_kernel<T, 4><<<g, kAppendThreads, 0, s>>>(c, b, x);
+  over_blocks(c, b, [&](dim3 g, int b0) {
+    if (n == 1) cache_append_kernel<T, 1><<<g, kAppendThreads, 0, s>>>(c, b, x, b0);
+    else if (n == 2) cache_append_kernel<T, 2><<<g, kAppendThreads, 0, s>>>(c, b, x, b0);
+    else cache_append_kernel<T, 4><<<g, kAppendThreads, 0, s>>>(c, b, x, b0);
+  });
+}
+
+template <class T>
+void launch_read_t(const CacheView &c, const BatchView &b, const OutKv &x, hipStream_t s) {
+  over_blocks(c, b, [&](dim3 g, int b0) { cache_read_kernel<T><<<g, 256, 0, s>>>(c, b, x, b0); });
 }
 
 }  // namespace
 
 hipError_t launch_cache_append(const CacheView &c, const BatchView &b, const void *k, const void *v, int type,
                                const int64_t *stride, hipStream_t s) {
-  const dim3 g(blocks_of(c, b), (unsigned)c.heads, (unsigned)b.requests * 2);
   const NewKv x{k, v, stride[0], stride[1], stride[2], stride[3]};
-  if (type == PALQ_F32) launch_append_t<F32>(g, c, b, x, s);
-  else if (type == PALQ_F16) launch_append_t<F16>(g, c, b, x, s);
-  else launch_append_t<BF16>(g, c, b, x, s);
+  if (type == PALQ_F32) launch_append_t<F32>(c, b, x, s);
+  else if (type == PALQ_F16) launch_append_t<F16>(c, b, x, s);
+  else launch_append_t<BF16>(c, b, x, s);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheView &c, const BatchView &b, void *k, void *v, int type, const int64_t *stride,
                              hipStream_t s) {
-  const dim3 g(blocks_of(c, b), (unsigned)c.heads, (unsigned)b.requests * 2);
   const OutKv x{k, v, stride[0], stride[1], stride[2], stride[3]};
-  if (type == PALQ_F32) cache_read_kernel<F32><<<g, 256, 0, s>>>(c, b, x);
-  else if (type == PALQ_F16) cache_read_kernel<F16><<<g, 256, 0, s>>>(c, b, x);
-  else cache_read_kernel<BF16><<<g, 256, 0, s>>>(c, b, x);
+  if (type == PALQ_F32) launch_read_t<F32>(c, b, x, s);
+  else if (type == PALQ_F16) launch_read_t<F16>(c, b, x, s);
+  else launch_read_t<BF16>(c, b, x, s);
   return hipGetLastError();
 }
 

@@ -94,27 +94,25 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const typename T::ra
 // piece, so a wave reads 64 bytes of 16 rows and writes a whole slab.
 __global__ __launch_bounds__(256) void slab_kernel(const int8_t *x, int64_t rows, int64_t slab_rows, int cols, int64_t ld,
                                                    int kp, int8_t *out) {
-  const int64_t slab = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int per = kp / 64;
-  const int64_t rt = slab / per;
-  if (rt >= slab_rows) return;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = rt * 16 + (lane & 15);
-  const int k = (int)(slab - rt * per) * 64 + (lane >> 4) * 16;
-  v4i o = {0, 0, 0, 0};
-  if (row < rows && k < cols) {
-    const int8_t *p = x + row * ld + k;
-    if (k + 16 <= cols) {
-      o = load_any(p);
-    } else {
+  const int per = kp / 64, lane = threadIdx.x & 63;
+  for (int64_t slab = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); slab < slab_rows * per; slab += (int64_t)gridDim.x * 4) {
+    const int64_t rt = slab / per, row = rt * 16 + (lane & 15);
+    const int k = (int)(slab - rt * per) * 64 + (lane >> 4) * 16;
+    v4i o = {0, 0, 0, 0};
+    if (row < rows && k < cols) {
+      const int8_t *p = x + row * ld + k;
+      if (k + 16 <= cols) {
+        o = load_any(p);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t c = (uint8_t)p[min(i, cols - 1 - k)];
-        o[i >> 2] |= k + i < cols ? (int)(c << (8 * (i & 3))) : 0;
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t c = (uint8_t)p[min(i, cols - 1 - k)];
+          o[i >> 2] |= k + i < cols ? (int)(c << (8 * (i & 3))) : 0;
+        }
       }
     }
+    *(v4i *)(out + slab * 1024 + lane * 16) = o;
   }
-  *(v4i *)(out + slab * 1024 + lane * 16) = o;
 }
 
 // ------------------------------------------------------------ few tokens
@@ -519,9 +517,12 @@ void launch_quantize_t(const void *x, int64_t rows, int cols, int64_t ld, int kp
     if (slabs) quantize_rows_kernel<T, 4, true><<<(unsigned)rows, 256, 0, s>>>((const R *)x, rows, cols, ld, kp, codes, codes_ld, scales);
     else quantize_rows_kernel<T, 4, false><<<(unsigned)rows, 256, 0, s>>>((const R *)x, rows, cols, ld, kp, codes, codes_ld, scales);
   } else {
-    const unsigned g = (unsigned)((rows + 3) / 4);
-    if (slabs) quantize_rows_kernel<T, 1, true><<<g, 256, 0, s>>>((const R *)x, rows, cols, ld, kp, codes, codes_ld, scales);
-    else quantize_rows_kernel<T, 1, false><<<g, 256, 0, s>>>((const R *)x, rows, cols, ld, kp, codes, codes_ld, scales);
+    for (int64_t r0 = 0; r0 < rows; r0 += 4 * kMaxGroups) {  // (slabs: fewer rows than that)
+      const int64_t n = std::min(rows - r0, 4 * kMaxGroups);
+      const unsigned g = (unsigned)((n + 3) / 4);
+      if (slabs) quantize_rows_kernel<T, 1, true><<<g, 256, 0, s>>>((const R *)x, rows, cols, ld, kp, codes, codes_ld, scales);
+      else quantize_rows_kernel<T, 1, false><<<g, 256, 0, s>>>((const R *)x + r0 * ld, n, cols, ld, kp, codes + r0 * codes_ld, codes_ld, scales + r0);
+    }
   }
 }
 
@@ -538,7 +539,7 @@ hipError_t launch_quantize_rows(const void *x, int type, int64_t rows, int cols,
 hipError_t launch_slabs(const int8_t *x, int64_t rows, int64_t padded_rows, int cols, int64_t ld, int kp, int8_t *out,
                         hipStream_t s) {
   const int64_t slabs = padded_rows / 16 * (kp / 64);
-  slab_kernel<<<(unsigned)((slabs + 3) / 4), 256, 0, s>>>(x, rows, padded_rows / 16, cols, ld, kp, out);
+  slab_kernel<<<(unsigned)std::min<int64_t>((slabs + 3) / 4, 1 << 16), 256, 0, s>>>(x, rows, padded_rows / 16, cols, ld, kp, out);
   return hipGetLastError();
 }
 

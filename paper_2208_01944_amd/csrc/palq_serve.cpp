@@ -364,7 +364,7 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
   AttendArgs a{view_of(cache), view_of(batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
                group, causal, window, scale, 0, 1, nullptr};
   if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
-  if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^31 or more workgroups");
+  if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^24 or more pairs of a request and a cache head");
   if (const size_t need = attend_work_bytes(a)) {
     a.part = (float *)workspace(ctx, need);
     if (!a.part) return fail(ctx, PALQ_ERR_NOMEM, "attention: workspace (in a capture: run the shape once before)");

@@ -124,6 +124,9 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t a) {
   return a;
 }
 
+// A launch has fewer than 2^32 threads along x: of 256 threads, this many workgroups at most.
+constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
+
 // A paged cache and a batch of requests as the kernels take them
 // (include/palq.h has their meaning).
 struct CacheView {

@@ -220,3 +220,84 @@ def test_lengths_near_the_limit(palq, length, heads, group, new):
         palq.attention(pair.gpu, q, out, b, 0.125, window=window)
         palq.sync()
         check_attend(pair, host(out), seen, [short], starts, host(q), 0.125, "bf16", causal=True, window=window)
+
+
+# ------------------------------------------------------------------ sizes of launches
+def test_quantize_rows_past_one_launch(palq):
+    """More rows than one launch has waves for."""
+    import torch
+    rows = (1 << 26) + 5
+    x = torch.randn(rows, 1, device="cuda", dtype=torch.float16)
+    x[::1000] = 0
+    codes, scales = torch.full((rows, 1), 99, dtype=torch.int8, device="cuda"), torch.full((rows,), -1.0, device="cuda")
+    palq.quantize_rows(x, codes, scales)
+    palq.sync()
+    v = x.cpu().numpy()[:, 0].astype(np.float32)
+    s = np.maximum(np.abs(v) * S.C127, S.FLOOR)
+    np.testing.assert_array_equal(scales.cpu().numpy(), s)
+    np.testing.assert_array_equal(codes.cpu().numpy()[:, 0], np.clip(np.rint(v * (np.float32(1) / s)), -127, 127).astype(np.int8))
+
+
+def test_linear_codes_past_one_grid(palq):
+    """More codes to lay out than the grid has waves: each takes several pieces."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    rows, n_in, n_out = 4200, 65500, 20
+    x = torch.randint(-128, 128, (rows, n_in), dtype=torch.int8, device="cuda")
+    w = torch.randint(-128, 128, (n_out, n_in), dtype=torch.int8, device="cuda")
+    lin = P.Linear(palq, w, torch.ones(n_out, device="cuda"), max_rows=rows)
+    y = torch.empty(rows, n_out, device="cuda")
+    lin.run(x, y, x_scale=torch.ones(rows, device="cuda"))
+    palq.sync()
+    want = torch.cat([torch.mm(part.double(), w.double().t().contiguous()) for part in x.split(600)]).float()  # (sums below 2^53)
+    assert torch.equal(y, want)
+
+
+def test_attention_bounds_past_one_launch(palq):
+    """A bound for a request's rows so loose that its workgroups, nearly all of them without rows, are more than one launch
+    takes: the same results as with the close bound, for wide and narrow pages."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    g = np.random.default_rng(8)
+    heads, dim, requests, new = 64, 64, 600, 100
+    for page in (16, 64):
+        per = -(-(new + 30) // page)
+        table, pages = g.permutation(requests * per).astype(np.int32).reshape(requests, per), requests * per
+        cache = P.Cache(*(torch.randint(-127, 128, s, dtype=torch.int8, device="cuda") for s in ((pages, heads, page, dim), (pages, heads, dim, page))),
+                        torch.rand(pages, heads, device="cuda") / 64, torch.rand(pages, heads, device="cuda") / 64)
+        lens, starts = g.integers(1, new + 30, requests).astype(np.int32), (np.arange(requests + 1) * new).astype(np.int32)
+        starts[1:] -= np.cumsum(g.integers(0, 2, requests)).astype(np.int32)
+        tokens = int(starts[-1])
+        assert -(-tokens // 128) * heads * requests > 1 << 24
+        q = torch.randn(tokens, heads, dim, device="cuda", dtype=torch.bfloat16)
+        outs = []
+        for max_new in (new, 1 << 29):
+            out = torch.full_like(q, 3.0)
+            palq.attention(cache, q, out, P.Batch(dev(table), dev(lens), dev(starts), max_new, per * page), 0.125)
+            palq.sync()
+            outs.append(out)
+        assert torch.equal(*outs) and torch.isfinite(outs[0]).all() and not (outs[0] == 3.0).all(2).any()
+
+
+def test_cache_bounds_past_one_launch(palq):
+    """Append and read of three tokens under bounds of 2^31 - 1 rows and tokens and a table of 2^24 pages."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    g = np.random.default_rng(9)
+    page, dim, room, length, new = 16, 64, 1 << 24, 35, 3
+    pair = Pair(P, 4, 2, page, dim)
+    small = np.int32([[2, 0, 3]])
+    pair.fill(g, small, None)
+    table = torch.full((1, room), -1, dtype=torch.int32, device="cuda")
+    table[:, :3] = dev(small)
+    b = P.Batch(table, dev(np.int32([length])), dev(np.int32([0, new])), (1 << 31) - 1, (1 << 31) - 1)
+    k, v = (g.standard_normal((new, 2, dim)).astype(np.float32) for _ in range(2))
+    pair.ref.append(small, [length], [0, new], k, v)
+    palq.cache_append(pair.gpu, dev(k), dev(v), b)
+    ok, ov = torch.zeros(new, 2, dim, device="cuda"), torch.zeros(new, 2, dim, device="cuda")
+    palq.cache_read(pair.gpu, ok, ov, b)
+    palq.sync()
+    pair.check(small, [length])
+    rk, rv = pair.ref.read(small, [length], [0, new])
+    np.testing.assert_array_equal(host(ok), rk)
+    np.testing.assert_array_equal(host(ov), rv)
