@@ -325,6 +325,7 @@ class Context:
         if codes.dtype != torch.int8 or tuple(codes.shape) != tuple(x.shape):
             raise PalqError(ERR_ARG, "codes must be int8 of x's shape")
         _need(scales, torch.float32, x.shape[0], "scales")
+        _on(self, x, codes, scales)
         xt, x_ld = _rows2(x)
         _, c_ld = _rows2(codes)
         self._check(_quantize_rows(self.h, x.data_ptr(), xt, x.shape[0], x.shape[1], x_ld, codes.data_ptr(), c_ld,
@@ -332,21 +333,21 @@ class Context:
 
     def cache_append(self, cache: Cache, k, v, batch: Batch):
         """palq_cache_append: k, v [tokens, heads, head_dim] into the pages of their requests."""
-        t, kr, kh, vr, vh = _pair3(k, v, batch, cache)
+        t, kr, kh, vr, vh = _pair3(self, k, v, batch, cache)
         st = _cache_append(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, t)
         if st:
             self._check(st)
 
     def cache_read(self, cache: Cache, k, v, batch: Batch):
         """palq_cache_read: the values of each request's last tokens into k, v [tokens, heads, head_dim]."""
-        t, kr, kh, vr, vh = _pair3(k, v, batch, cache)
+        t, kr, kh, vr, vh = _pair3(self, k, v, batch, cache)
         st = _cache_read(self.h, cache.ref, batch.ref, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, t)
         if st:
             self._check(st)
 
     def attention(self, cache: Cache, q, out, batch: Batch, scale, causal=True, window=0):
         """palq_attention: q, out [tokens, q_heads, head_dim]."""
-        t, qr, qh, orow, oh = _pair3(q, out, batch, cache, True)
+        t, qr, qh, orow, oh = _pair3(self, q, out, batch, cache, True)
         st = _attention(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, t, scale, causal,
                         window)
         if st:
@@ -365,6 +366,8 @@ class Linear:
         _need(w_scale, torch.float32, self.n_out, "w_scale")
         if bias is not None:
             _need(bias, torch.float32, self.n_out, "bias")
+            _on(ctx, bias)
+        _on(ctx, w, w_scale)
         _, w_ld = _rows2(w)
         h = c_p()
         ctx._check(_linear_create(ctx.h, w.data_ptr(), w_ld, w_scale.data_ptr(), _ptr(bias), self.n_out, self.n_in, max_rows,
@@ -381,8 +384,12 @@ class Linear:
             raise PalqError(ERR_ARG, "x or y does not have the layer's shape")
         xt, x_ld = _rows2(x)
         yt, y_ld = _rows2(y)
+        d = self.ctx.device
+        if d >= 0 and (x.get_device() != d or y.get_device() != d):
+            _on(self.ctx, x, y)
         if x_scale is not None:
             _need(x_scale, torch.float32, rows, "x_scale")
+            _on(self.ctx, x_scale)
             x_scale = x_scale.data_ptr()
         st = _linear_run(self.ctx.h, self.h, x.data_ptr(), xt, x_ld, x_scale, rows, y.data_ptr(), yt, y_ld)
         if st:
@@ -408,6 +415,7 @@ class Cache:
             raise PalqError(ERR_ARG, "k and v must be contiguous")
         _need(k_scale, torch.float32, pages * heads, "k_scale")
         _need(v_scale, torch.float32, pages * heads, "v_scale")
+        self.device = _together(k, v, k_scale, v_scale)
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.heads, self.page, self.dim = pages, heads, page, dim
         self.desc = CacheDesc(pages, page, heads, dim, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
@@ -432,6 +440,7 @@ class Batch:
             raise PalqError(ERR_ARG, "table must be contiguous int32")
         _need(lens, torch.int32, requests, "lens")
         _need(starts, torch.int32, requests + 1, "starts")
+        self.device = _together(table, lens, starts)
         self.table, self.lens, self.starts, self.tokens = table, lens, starts, 0
         self.desc = BatchDesc(requests, max_pages, table.data_ptr(), lens.data_ptr(), starts.data_ptr(), 0, max_new, max_len)
         self.ref = ctypes.byref(self.desc)
@@ -440,6 +449,24 @@ class Batch:
 def _need(t, dtype, n, what):
     if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise PalqError(ERR_ARG, f"{what} must be {n} contiguous values of {dtype}")
+
+
+def _on(ctx, *tensors):
+    """A kernel reads whatever address it is given: tensors have to be on the context's device (no matter where for a
+    validate-only one)."""
+    d = ctx.device
+    if d >= 0:
+        for t in tensors:
+            if t.get_device() != d:
+                raise PalqError(ERR_ARG, f"a tensor is on {t.device}, the context on cuda:{d}")
+
+
+def _together(*tensors):
+    """The one device of some tensors (-1: the host)."""
+    d = tensors[0].get_device()
+    if any(t.get_device() != d for t in tensors):
+        raise PalqError(ERR_ARG, "the tensors are on different devices")
+    return d
 
 
 def _rows2(t):
@@ -454,7 +481,7 @@ def _rows2(t):
     return kind, (ld if rows > 1 else max(ld, cols))
 
 
-def _pair3(a, b, batch, cache, query=False):
+def _pair3(ctx, a, b, batch, cache, query=False):
     """Type, and row and head strides of both, of two [tokens, heads, head_dim]
     tensors of a batch (query: of any multiple of the cache's heads)."""
     tokens, heads, dim = a.shape
@@ -465,6 +492,9 @@ def _pair3(a, b, batch, cache, query=False):
         raise PalqError(ERR_ARG, "the tensors differ in type or shape, or have no element type of the library")
     if a1 != 1 or b1 != 1 or dim != cache.dim or (heads % cache.heads if query else heads != cache.heads):
         raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim] of the cache, a head's channels consecutive")
+    d = ctx.device
+    if d >= 0 and not (a.get_device() == d and b.get_device() == d and cache.device == d and batch.device == d):
+        raise PalqError(ERR_ARG, f"tensors, cache or batch are not on the context's device, cuda:{d}")
     if batch.tokens != tokens:
         batch.tokens = batch.desc.tokens = tokens
     return kind, ar, ah, br, bh
