@@ -178,7 +178,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   const int h = blockIdx.y, r = blockIdx.z, split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
   const CacheView &cv = a.c;
   const int heads = cv.heads;
-  const Request q = request_of(a.b, r, cv.shift);
+  const Request q = request_of(a.b, r);
   const int rows = q.n * a.group, first = rt * NQ * 16;
   if (first >= rows) return;
   const int last = min(rows, first + NQ * 16) - 1;
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   const int combo = blockIdx.x % combos, rest = blockIdx.x / combos;
   const int h = combo % heads, r = (combo / heads + rest) % a.b.requests, split = rest % a.splits, rt = first_tile + row_tiles - 1 - rest / a.splits;
   const CacheView &cv = a.c;
-  const Request q = request_of(a.b, r, cv.shift);
+  const Request q = request_of(a.b, r);
   const int rows = q.n * a.group, first = rt * ROWS;
   if (first >= rows) return;
   const int last = min(rows, first + ROWS) - 1;
@@ -841,7 +841,7 @@ template <class T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int W = D / 4;
   const int r = blockIdx.y;
-  const Request q = request_of(a.b, r, a.c.shift);
+  const Request q = request_of(a.b, r);
   const int hs = a.c.heads * a.group, sub = threadIdx.x / W, d = threadIdx.x % W * 4;
   const int64_t i = (int64_t)blockIdx.x * (256 / W) + sub;
   if (sub >= 256 / W || i >= (int64_t)q.n * hs) return;

@@ -60,14 +60,14 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(CacheView 
   __shared__ uint32_t turned[turned_words(NI)];  // [dim][turned_stride]
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
-  const Request q = request_of(b, r, c.shift);
-  const int old = max(0, q.pos);  // rows before position 0 have no place
+  const Request q = request_of(b, r);
+  const int old = max(0, q.pos), stop = min(q.len, q.pos + q.n);  // rows before position 0 have no place
   const int block = (old >> c.shift) + block0 + (int)blockIdx.x;
-  const int64_t t0 = (int64_t)block << c.shift, lo = max((int64_t)old, t0), hi = min((int64_t)min(q.len, q.pos + q.n), t0 + c.page);
-  if (lo >= hi) return;
+  if (old >= stop || block > (stop - 1) >> c.shift) return;
+  const int t0 = block << c.shift, lo = max(old, t0), hi = min(stop, t0 + c.page);
   const int pid = page_of(c, b, r, block);
   if (pid < 0) return;
-  const int kept = (int)(lo - t0), end = (int)(hi - t0), D = c.dim, groups = D / 8, items = append_items(c.page, D);
+  const int kept = lo - t0, end = hi - t0, D = c.dim, groups = D / 8, items = append_items(c.page, D);
   const R *src = (const R *)(values ? x.v : x.k);
   const int64_t row = values ? x.v_row : x.k_row, head = values ? x.v_head : x.k_head;
   src += (q.row0 + (t0 - q.pos)) * row + h * head;  // row of token t0 (there may be none)
@@ -173,12 +173,12 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheView c, BatchView 
   typedef typename T::raw R;
   const int r = blockIdx.z >> 1, h = blockIdx.y;
   const bool values = blockIdx.z & 1;
-  const Request q = request_of(b, r, c.shift);
-  const int first = max(0, q.pos);
+  const Request q = request_of(b, r);
+  const int first = max(0, q.pos), stop = min(q.len, q.pos + q.n);
   const int block = (first >> c.shift) + block0 + (int)blockIdx.x;
-  const int64_t t0 = (int64_t)block << c.shift, lo = max((int64_t)first, t0), hi = min((int64_t)min(q.len, q.pos + q.n), t0 + c.page);
-  if (lo >= hi) return;
-  const int from0 = (int)(lo - t0), end = (int)(hi - t0);  // the block's tokens that are read
+  if (first >= stop || block > (stop - 1) >> c.shift) return;
+  const int t0 = block << c.shift, lo = max(first, t0), hi = min(stop, t0 + c.page);
+  const int from0 = lo - t0, end = hi - t0;  // the block's tokens that are read
   const int pid = page_of(c, b, r, block), D = c.dim;
   const int64_t ph = (int64_t)max(pid, 0) * c.heads + h;
   const float s = pid < 0 ? 0.0f : (values ? c.vs : c.ks)[ph];

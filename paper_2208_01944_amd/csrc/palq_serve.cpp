@@ -160,8 +160,10 @@ CacheView view_of(const palq_cache *c) {
   while ((1 << v.shift) < v.page) ++v.shift;
   return v;
 }
-BatchView view_of(const palq_batch *b) {
-  return BatchView{b->table, b->lens, b->starts, b->requests, b->max_pages, b->max_new, b->tokens, b->max_len};
+BatchView view_of(const palq_cache *c, const palq_batch *b) {
+  const int64_t limit = std::min(std::min((int64_t)b->max_pages * c->page_tokens, (int64_t)b->max_len), kMaxTokens);
+  return BatchView{b->table, b->lens, b->starts, b->requests, b->max_pages, b->max_new, b->tokens, b->max_len,
+                   (int32_t)std::min(b->tokens, (int64_t)0x7fffffff), (int32_t)limit};
 }
 
 }  // namespace
@@ -305,7 +307,7 @@ palq_status palq_cache_append(palq_ctx *ctx, const palq_cache *cache, const palq
     return PALQ_OK;
   hipSetDevice(ctx->device);
   const int64_t stride[4] = {k_row, k_head, v_row, v_head};
-  const hipError_t e = launch_cache_append(view_of(cache), view_of(batch), k, v, type, stride, ctx->stream);
+  const hipError_t e = launch_cache_append(view_of(cache), view_of(cache, batch), k, v, type, stride, ctx->stream);
   return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "cache append");
 }
 
@@ -332,7 +334,7 @@ palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_b
     return PALQ_OK;
   hipSetDevice(ctx->device);
   const int64_t stride[4] = {k_row, k_head, v_row, v_head};
-  const hipError_t e = launch_cache_read(view_of(cache), view_of(batch), k, v, type, stride, ctx->stream);
+  const hipError_t e = launch_cache_read(view_of(cache), view_of(cache, batch), k, v, type, stride, ctx->stream);
   return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "cache read");
 }
 
@@ -361,7 +363,7 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
   if ((st = check_written(ctx, cache, out, batch->tokens, out_row, out_head, q_heads, type))) return st;
   if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0) return PALQ_OK;
   hipSetDevice(ctx->device);
-  AttendArgs a{view_of(cache), view_of(batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
+  AttendArgs a{view_of(cache), view_of(cache, batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
                group, causal, window, scale, 0, 1, nullptr};
   if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
   if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^24 or more pairs of a request and a cache head");

@@ -138,23 +138,24 @@ struct BatchView {
   const int32_t *table, *lens, *starts;
   int32_t requests, max_pages, max_new;
   int64_t tokens, max_len;
+  int32_t rows, limit;  // tokens, and the most that a request holds, in 32 bits
 };
 
 // One request: `n` ragged rows from row0 on, at positions pos, pos + 1, .., and `len`
 // tokens.  Whatever the arrays hold, len stays inside the table and the rows
 // inside the tensors; what is left out (rows or tokens past the bounds) does not
-// move the others, so pos follows from lens and starts as they are.
+// move the others: row i of the tensors is at lens[r] - starts[r + 1] + i.  In 32 bits,
+// so that it stays in scalar registers; pos wraps round only where n or len is 0.
 struct Request { int64_t row0; int32_t n, len, pos; };
 constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 1024;  // so that the tiles that are asked for past a request's end have 32-bit places
-__device__ __forceinline__ Request request_of(const BatchView &b, int r, int shift) {
+__device__ __forceinline__ Request request_of(const BatchView &b, int r) {
+  const int32_t s0 = b.starts[r], s1 = b.starts[r + 1], all = b.lens[r];
+  const int32_t row0 = max(s0, 0), end = min(s1, b.rows);
   Request q;
-  const int64_t s0 = b.starts[r], s1 = b.starts[r + 1], all = b.lens[r];
-  const int64_t skip = s0 < 0 ? -s0 : 0;  // rows before the tensors' first
-  q.row0 = s0 + skip;
-  const int64_t pos = all - (s1 - s0) + skip;
-  q.pos = (int32_t)min(max(pos, (int64_t)-0x7fffffff), (int64_t)0x7fffffff);  // (no row reaches 0 from the one end, there are none at the other)
-  q.n = (int32_t)max((int64_t)0, min(min(s1, b.tokens) - q.row0, b.max_new - skip));
-  q.len = (int32_t)max((int64_t)0, min(min(all, kMaxTokens), min((int64_t)b.max_pages << shift, b.max_len)));
+  q.row0 = row0;
+  q.n = end > row0 ? max(0, min(end - row0, b.max_new + min(s0, 0))) : 0;  // (max_new counts from starts[r])
+  q.len = max(0, min(all, b.limit));
+  q.pos = (int32_t)((uint32_t)all - (uint32_t)s1 + (uint32_t)row0);
   return q;
 }
 
