@@ -288,6 +288,16 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     for (int s = 0; s < KS; ++s) Q[n][s] = scaled<T>(raw[n][s], rs.in);
     f[n] = rs.out * kLog2e * fabsf(a.scale);
   }
+  // the largest exponent of the present tile's scales
+  auto most_of = [&](bool there, float vst) __attribute__((always_inline)) {
+    const int ve = there ? exponent_of(vst) : kNoUnit;
+    return max(max(__builtin_amdgcn_readlane(ve, 0), __builtin_amdgcn_readlane(ve, 16)),
+               max(__builtin_amdgcn_readlane(ve, 32), __builtin_amdgcn_readlane(ve, 48)));
+  };
+  if (tb + wave < te) {  // (here the operands are still on their way)
+    const int first_most = most_of(vthere, vs);
+    if (unit.leaves<4>(first_most)) unit.follow<4>(first_most);
+  }
   auto step = [&](int tile, auto last) __attribute__((always_inline)) {
     constexpr bool more = !decltype(last)::value;
     const int vt = tile * 64 + vc;
@@ -296,9 +306,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     // (no scale of the tile from 2^5 on, one from 2^-4 on: the unit stays)
     float vq = __builtin_ldexpf(vst, -unit.u);
     if (__any(there & (vq >= 32.0f)) || !__any(there & (vq >= 0.0625f))) {
-      const int ve = there ? exponent_of(vst) : kNoUnit, was = unit.u;
-      const int most = max(max(__builtin_amdgcn_readlane(ve, 0), __builtin_amdgcn_readlane(ve, 16)),
-                           max(__builtin_amdgcn_readlane(ve, 32), __builtin_amdgcn_readlane(ve, 48)));
+      const int most = most_of(there, vst), was = unit.u;
       if (unit.leaves<4>(most)) unit.follow<4>(most);
       const float by = __builtin_ldexpf(1.0f, was - unit.u);
 #pragma unroll
