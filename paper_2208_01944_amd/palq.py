@@ -33,6 +33,7 @@ OP_CONV, OP_MAXPOOL, OP_AVGSUM, OP_FC, OP_SHUFFLE_MODULE, OP_CHANNEL_SHUFFLE = 1
 NET_KEEP_ALL, NET_TIMING, NET_GRAPH, NET_PIXEL_LAYOUT = 1, 2, 4, 8
 LAYOUT_PIXEL, LAYOUT_GROUP = 0, 1
 F32, F16, BF16, I8 = 0, 1, 2, 3  # element types of the transformer operators
+_INT_MAX = (1 << 31) - 1
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
 
 
@@ -326,6 +327,8 @@ class Context:
             raise PalqError(ERR_ARG, "codes must be int8 of x's shape")
         _need(scales, torch.float32, x.shape[0], "scales")
         _on(self, x, codes, scales)
+        if x.shape[1] > _INT_MAX:
+            raise PalqError(ERR_UNSUPPORTED, "a row of 2^31 elements or more")
         xt, x_ld = _rows2(x)
         _, c_ld = _rows2(codes)
         self._check(_quantize_rows(self.h, x.data_ptr(), xt, x.shape[0], x.shape[1], x_ld, codes.data_ptr(), c_ld,
@@ -348,8 +351,10 @@ class Context:
     def attention(self, cache: Cache, q, out, batch: Batch, scale, causal=True, window=0):
         """palq_attention: q, out [tokens, q_heads, head_dim]."""
         t, qr, qh, orow, oh = _pair3(self, q, out, batch, cache, True)
+        if window < 0:
+            raise PalqError(ERR_ARG, "window must be 0 or more")
         st = _attention(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, t, scale, causal,
-                        window)
+                        min(window, _INT_MAX))
         if st:
             self._check(st)
 
@@ -440,6 +445,9 @@ class Batch:
             raise PalqError(ERR_ARG, "table must be contiguous int32")
         _need(lens, torch.int32, requests, "lens")
         _need(starts, torch.int32, requests + 1, "starts")
+        if max_new < 0 or max_len < 0:
+            raise PalqError(ERR_ARG, "max_new and max_len must be 0 or more")
+        max_new, max_len = min(max_new, _INT_MAX), min(max_len, _INT_MAX)
         self.device = _together(table, lens, starts)
         self.table, self.lens, self.starts, self.tokens = table, lens, starts, 0
         self.desc = BatchDesc(requests, max_pages, table.data_ptr(), lens.data_ptr(), starts.data_ptr(), 0, max_new, max_len)
