@@ -742,7 +742,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
         }
       }
     }
-    // s fk, fk >= 0: the largest comes from the largest product (of the scores alone: a wide tile's lv is up to 5)
+    // s fk + lv, fk >= 0: the largest comes from the largest product.  Of lv only the fraction, so that a
+    // wide tile's whole powers of two (up to 4) take nothing from the others, and the largest weight is a
+    // power of two, which fp16 holds exactly: rows with few tokens gain most.
     const float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
     float mx = -INFINITY;
 #pragma unroll
@@ -750,7 +752,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       float m = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 16; ++j) m = fmaxf(m, S[u][j]);
-      mx = fmaxf(mx, m == -INFINITY ? -INFINITY : m * fk[u]);
+      mx = fmaxf(mx, m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[u], __builtin_amdgcn_fractf(lv[u])));
     }
     mx = other_half_max(mx);
     if (__any(mx > M + kSlack)) {

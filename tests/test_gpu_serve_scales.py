@@ -173,3 +173,23 @@ def test_attention_scales_of_the_scores_near_the_ends(palq, shape, scale):
     palq.attention(pair.gpu, q, out, b, scale)
     palq.sync()
     check_channels(pair, host(out), table, lens, starts, host(q), scale, "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("page,dim", [(16, 64), (64, 128), (32, 96), (128, 64)])
+@pytest.mark.parametrize("shape", ["rows16", "rows32", "splits", "tiles"])
+def test_attention_of_one_token_is_its_value(palq, shape, page, dim, dtype):
+    """A row that sees one token gives its value: the largest weight of a row is held exactly, so that the result has the
+    rounding to its type and the fp32 errors of one logarithm, two powers and a division (below 2^-18) alone."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("one token", shape, page, dim, dtype)
+    g, pair, table, lens, starts, q, b = case(P, shape, page, dim, 7)
+    pair.fill(g, table, lens)
+    q = q.to(torch.float16 if dtype == "f16" else torch.bfloat16)
+    out = torch.full_like(q, 3.0)
+    palq.attention(pair.gpu, q, out, b, 0.125, window=1)
+    palq.sync()
+    ref = pair.ref.attend(table, lens, starts, host(q), 0.125, True, 1)[0]
+    err = np.abs(host(out) - ref)
+    assert (err <= (EPS[dtype] * (1 + 2.0 ** -10) + 2.0 ** -18) * np.abs(ref) + TINY[dtype]).all()
