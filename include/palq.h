@@ -443,8 +443,9 @@ palq_status palq_net_reset_times(palq_net *net);
  * a block (the tokens of one cache page, one head):
  *   a = max |x|;  s = max(a * fl(1/127), 2^-100);
  *   code = clamp(rint(x * fl(1/s)), -127, 127), ties to even.
- * A row or block with an element that is not finite has scale NaN and its
- * codes are 0, so the results that depend on it, and no others, are NaN.
+ * A row, or new tokens of a block, with an element that is not finite give
+ * scale NaN and codes 0, so the results that depend on them, and no others,
+ * are NaN.  A block keeps a NaN until its page starts afresh.
  */
 #define PALQ_F32 0
 #define PALQ_F16 1

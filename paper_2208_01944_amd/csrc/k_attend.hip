@@ -165,8 +165,8 @@ __device__ __forceinline__ h8 scaled(v4i raw, float f) {
 // NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
 // fourth tile of 64 tokens; the waves join in LDS, splits in attend_join_kernel.
 // Operands go from memory straight into registers, one tile ahead.  32 requests of 2047
-// to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 118 us, 5.1 TB/s (a
-// plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 20 us.
+// to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 115 us, 5.3 TB/s (a
+// plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 21 us.
 template <class T, int D, int NQ>
 __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     if constexpr (more) load_k(tile + 4);
     h8 P[NQ][2];
     // Tokens that all rows see need no masks (columns past the last row are not stored).
-    // 8 requests of 17 to 131 rows, heads of 64: 17.7 us, 19.9 with masks always.  The wider
+    // 8 requests of 17 to 131 rows, heads of 64: 18.5 us, 21.5 with masks always.  The wider
     // builds keep them: two paths took 256 registers and scratch (heads of 128, 32 rows).
     const bool whole = D * NQ <= 128 && __all(there) && tile * 64 >= rl.lo && tile * 64 + 64 <= rf.hi;
     auto weigh = [&](int n, auto masks) __attribute__((always_inline)) {
@@ -455,9 +455,9 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 // as codes a tile ahead, converted to fp16 once and kept in LDS for all waves, one
 // barrier a tile; two workgroups on a CU (up to 128 channels) fill each other's gaps.
 // 4 requests, 1531 to 2048 tokens behind cached ones, 2100 to 4096 in all, 8 heads of
-// 128, group 4: 320 us, 775 TFLOP/s (a bf16 library product of 8192^3: 1240).  A wave's
-// step of 64 tokens takes about 4000 cycles alone, 1024 of them products; without the
-// softmax the time falls by 7 %, without the conversion by 27 %.
+// 128, group 4: 324 us, 766 TFLOP/s (a bf16 library product of 8192^3: 1240 to 1270).  A
+// wave's step of 64 tokens takes about 4000 cycles alone, 1024 of them products; the softmax
+// is 28 % of the time (234 us without), the conversion 8 % (298).
 //
 // LDS holds each matrix operand as the 1 KB that a wave reads, lane after lane, so
 // a read is a lane's own address plus a constant and meets no bank twice; the
@@ -478,7 +478,7 @@ struct TileLds {
 
 // Keeps kAhead operand reads in flight before the N products of this block: an LDS
 // read takes the time of four products, and the compiler by itself asks for one
-// operand at a time (4 requests, 2048 tokens of 4096: 472 us, 516 without).
+// operand at a time (4 requests, 2048 tokens of 4096: 451 us, 458 without).
 constexpr int kAhead = 5;
 template <int N>
 __device__ __forceinline__ void ahead() {
@@ -899,7 +899,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // While the small blocks are at most 3 for each CU, their many waves over the
 // tokens end sooner than the tile kernel's long chain of steps, although each
 // block converts its codes itself: 4 requests, 8 heads, group 4, 2048 tokens, 64 /
-// 128 / 256 new ones: 30 / 44 / 79 us against 64 / 66 / 70.
+// 128 / 256 new ones: 30 / 40 / 72 us against 36 / 40 / 58.
 int block_rows(const AttendArgs &a, int cus) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
   return (rows + small - 1) / small * a.c.heads * a.b.requests <= 3 * cus ? (int)small : 128;
@@ -946,7 +946,7 @@ bool attend_plan(AttendArgs &a, int cus) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
   const int64_t base = std::max<int64_t>(1, rt * a.c.heads * a.b.requests);
   // Parts of a request's tokens, until two workgroups stand on every CU (one of 32
-  // rows: its waves hold twice the accumulators; 4 requests, 5 tokens, window 8191: 23 us
+  // rows: its waves hold twice the accumulators; 4 requests, 5 tokens, window 8191: 24 us
   // in 8 parts, 26 in 16).  A part has two tiles or more for every wave, and what is
   // done in four is not cut at all: joining costs as much.
   const int64_t most = a.b.max_len <= 1024 ? 1 : (a.b.max_len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;

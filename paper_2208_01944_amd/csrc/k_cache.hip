@@ -10,9 +10,10 @@
 // 16 consecutive bytes.
 //
 // Both directions are bound by memory: a workgroup takes one (request, block,
-// head, keys or values).  8 prompts of 113 to 2048 tokens, 8 heads of 128, bf16: append 21
-// us (53 MB, 2.5 TB/s), read back as fp32 19 us (89 MB, 4.7 TB/s); 64 single tokens 6 us,
-// four loads that wait for each other (lengths, table, scale, values).
+// head, keys or values).  8 prompts of 113 to 2048 tokens, 8 heads of 128, bf16: append 20
+// us (53 MB, 2.6 TB/s), read back as fp32 18 us (89 MB, 4.9 TB/s); 64 single tokens 6 us
+// and, their blocks read back, 10: four loads that wait for each other (lengths, table, scale,
+// values).
 #include <algorithm>
 
 #include "cache.h"

@@ -24,7 +24,7 @@ namespace {
 // consecutive columns at a time and keeps the first kHeld such pieces in
 // registers between the two looks at a row (largest magnitude, then codes): 8192
 // columns of one wave, 16384 of four.  4096 rows of 8192
-// bf16: 21 us.
+// bf16 (100 MB): 26 us from memory, 22 when the rows are in the caches.
 
 template <class T, int WPR, bool SLABS>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const typename T::raw *x, int64_t rows, int cols, int64_t ld,
@@ -196,9 +196,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void linear_few_kernel(LinearArg
 // One token of floating values: every workgroup quantises the row by itself, into
 // LDS, while its first weights are on their way; one launch instead of two.  It goes
 // through its 16-channel tiles with the same row.  At most 128 registers, so that two
-// workgroups on a CU keep twice the weights in flight.  4096 x 4096 weights 4.9 us (7.2
-// with the quantiser apart), 8192 x 8192 12.1 us, 5.5 TB/s.  (Three rows this way need
-// 156 registers: 8192 x 8192 17.8 us, against 15.6 in two launches.)
+// workgroups on a CU keep twice the weights in flight.  A call with 4096 x 4096 weights 5.2
+// us (7.5 with the quantiser in a launch of its own), 6.8 (8.8) with weights from memory;
+// 8192 x 8192 12.3 (15.6), 14.8 (19.7) from memory.  (Three rows this way need 156
+// registers and were slower than two launches, 17.8 us against 15.6.)
 struct RawRow { const void *x; int32_t n_in; };
 constexpr int kOneBytes = 16 << 10;  // at most: bytes of the row's codes
 
@@ -274,8 +275,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void linear_one_kernel(LinearArg
 // both operands' slabs are copied from memory straight into LDS (two stages, one
 // in use, one on its way), and a wave reads the operands of the next 32 k while
 // the matrix cores work on the present ones, across the stage's barrier too.  4096 rows,
-// 8192 x 8192 weights: 230 us, 2.4 POP/s, as the library's int8 product (2.39; its
-// codes come ready); the matrix cores are busy 65 % of the time at 1.7 GHz, to which
+// 8192 x 8192 weights: 231 us at best and 243 in the middle of 40 under the profiler, 2.38 and 2.26
+// POP/s (the library's int8 product: 2.41 to 2.45; its codes come ready); the matrix cores are busy 65 % of the time at 1.7 GHz, to which
 // operands of random codes bring the clock down (all-zero codes: 184 us).
 // 16 bytes per lane from the buffer into LDS at `dst` (uniform) + 16 lane; in asm,
 // so that the compiler does not order LDS reads after them: the stages' waits and
