@@ -90,30 +90,25 @@ __device__ __forceinline__ int exponent_of(float s) {  // of a normal number; kN
 }
 struct Unit {
   int u = kNoUnit, top = kNoUnit;
-  // e: the largest exponent of a tile's scales.  It stays within [u - BELOW, u + 4], and u within 72 of the
-  // largest e so far (2^72, weights of 2^13, codes of 2^7 and 2^31 tokens: sums stay in fp32).
-  template <int BELOW>
-  __device__ __forceinline__ bool leaves(int e) const { return e != kNoUnit && (e > u + 4 || e < u - BELOW); }
-  template <int BELOW>
-  __device__ __forceinline__ void follow(int e) {
+  // To n, or to 2^-72 of the largest scale so far where that is more (2^72, weights of 2^13, codes of 2^7 and
+  // 2^31 tokens: sums stay in fp32); e: the tile's largest exponent.
+  __device__ __forceinline__ void move(int n, int e) {
     top = max(top, e);
-    u = max(BELOW ? e : e - 2, top - 72);
+    u = max(n, top - 72);
   }
+  // Keeps e within [u - 4, u + 4].
+  __device__ __forceinline__ bool leaves(int e) const { return e != kNoUnit && (e > u + 4 || e < u - 4); }
 };
 // Scale over unit, q = vs / 2^U: its power of two 2^a goes into the codes (two halves of m, and of n = -1152 m), the
-// rest into the exponent (u, and 1 / r).
+// rest into the exponent (u, and 1 / r).  whole: all of it goes into the exponent.
 struct ValueScale { float u, rv; uint32_t m, n; };
-__device__ __forceinline__ ValueScale value_scale(float q) {
-  const float p = fminf(fmaxf(__uint_as_float(__float_as_uint(q) & 0x7f800000u), 5.9604645e-8f), 16.0f);  // 2^-24 .. 2^4
+__device__ __forceinline__ ValueScale value_scale(float q, bool whole = false) {
+  const float pow2 = fminf(fmaxf(__uint_as_float(__float_as_uint(q) & 0x7f800000u), 5.9604645e-8f), 16.0f);  // 2^-24 .. 2^4
+  const float p = whole ? 1.0f : pow2;
   const float r = q * __builtin_amdgcn_rcpf(p), l = __builtin_amdgcn_logf(r), u = l < -64.0f ? -64.0f : l;  // (NaN stays)
   const float f = q == 0.0f ? 0.0f : p;
   const h2 m = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(f, f)), n = m * h2{(_Float16)-1152.0f, (_Float16)-1152.0f};
   return {u, exp2_fast(-u), __builtin_bit_cast(uint32_t, m), __builtin_bit_cast(uint32_t, n)};
-}
-// Where the whole tile has one scale, all of it goes into the exponent.
-__device__ __forceinline__ ValueScale value_scale_whole(float q) {
-  const float l = __builtin_amdgcn_logf(q), u = l < -64.0f ? -64.0f : l;
-  return {u, exp2_fast(-u), 0u, 0u};
 }
 
 // One row's reach: tokens [lo, hi).
@@ -296,7 +291,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   };
   if (tb + wave < te) {  // (here the operands are still on their way)
     const int first_most = most_of(vthere, vs);
-    if (unit.leaves<4>(first_most)) unit.follow<4>(first_most);
+    if (first_most != kNoUnit) unit.move(first_most, first_most);
   }
   auto step = [&](int tile, auto last) __attribute__((always_inline)) {
     constexpr bool more = !decltype(last)::value;
@@ -307,7 +302,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     float vq = __builtin_ldexpf(vst, -unit.u);
     if (__any(there & (vq >= 32.0f)) || !__any(there & (vq >= 0.0625f))) {
       const int most = most_of(there, vst), was = unit.u;
-      if (unit.leaves<4>(most)) unit.follow<4>(most);
+      if (unit.leaves(most)) unit.move(most, most);
       const float by = __builtin_ldexpf(1.0f, was - unit.u);
 #pragma unroll
       for (int n = 0; n < NQ; ++n)
@@ -478,8 +473,10 @@ struct TileLds {
 
 // Keeps kAhead operand reads in flight before the N products of this block: an LDS
 // read takes the time of four products, and the compiler by itself asks for one
-// operand at a time (4 requests, 2048 tokens of 4096: 451 us, 458 without).
-constexpr int kAhead = 5;
+// operand at a time (4 requests, 2048 tokens of 4096: 451 us, 458 without).  With one more in
+// flight the narrow pages' build for heads of 128 has no registers left for any: 153 us become
+// 167 (4 requests, 900 to 1100 tokens of 2048, pages of 32).
+constexpr int kAhead = 4;
 template <int N>
 __device__ __forceinline__ void ahead() {
   __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);  // LDS reads
@@ -497,8 +494,8 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + kTileThreads - 1) / kTileThreads;
   __shared__ __attribute__((aligned(256))) uint8_t lds[G::BYTES];
   __shared__ float4 blocks[4][4];  // of four tiles' 16-token chunks: {ks, u, 1 / r, page there}
-  __shared__ uint2 factors[4][4];  // narrow pages: and the factor of their values' codes (m, n)
-  __shared__ int units[4];         // and the tiles' units
+  __shared__ uint32_t factors[4][4];  // narrow pages: and the factor of their values' codes
+  __shared__ int units[4];            // and the tiles' units
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, c = lane >> 5;
   // cache heads go fastest, so a head's tiles share one XCD's L2 where heads are a
   // multiple of 8; the rows with the longest reach start first
@@ -613,28 +610,36 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   // next.  Loads end in order, so the entries that the next call needs come first.
   // None of it stands under a condition, so that waits count only what they need; past
   // the last tile it reads tiles that nobody uses.  par: p - tb is odd.
-  // WIDE: one scale a tile, which every wave follows in scalar registers (the units of two
-  // tiles, by their parity); else wave 0 follows the largest, and the others read LDS.
+  // The units of two tiles, by their parity, in scalar registers.  WIDE: one scale a tile,
+  // which every wave follows; else wave 0 follows the four chunks', and the others read LDS
+  // after a step's barrier for the next step, with the factor of this thread's 16 tokens.
   Unit unit;
-  int wide_unit[2] = {kNoUnit, kNoUnit};
+  int tile_unit[2] = {kNoUnit, kNoUnit}, next_unit = kNoUnit;
+  uint32_t factor = 0;
+  auto see_blocks = [&](int p) __attribute__((always_inline)) {
+    if constexpr (!WIDE) {
+      next_unit = units[(p - tb) & 3];
+      factor = factors[(p - tb) & 3][threadIdx.x >> 4 & 3];  // (a thread's pieces are 256 apart: the same tokens)
+    }
+  };
   auto bring_blocks = [&](int p, auto par) __attribute__((always_inline)) {
     if constexpr (WIDE) {
       const int e = valid(ent[decltype(par)::value].b) ? exponent_of(bvs) : kNoUnit;
-      if (unit.leaves<0>(e)) unit.follow<0>(e);
-      wide_unit[decltype(par)::value] = unit.u;
+      if (e != kNoUnit && (e < unit.u || e > unit.u + 4)) unit.move(e - 2, e);
+      tile_unit[decltype(par)::value] = unit.u;
       if (wave == 0 && lane < 4) {
-        const ValueScale v = value_scale_whole(__builtin_ldexpf(bvs, -unit.u));
+        const ValueScale v = value_scale(__builtin_ldexpf(bvs, -unit.u), true);
         blocks[(p - tb) & 3][lane] = make_float4(bks, v.u, v.rv, bthere);
       }
     } else if (wave == 0) {
       const int e = bthere != 0.0f ? exponent_of(bvs) : kNoUnit;
-      const int most = max(max(__builtin_amdgcn_readlane(e, 0), __builtin_amdgcn_readlane(e, 1)),
-                           max(__builtin_amdgcn_readlane(e, 2), __builtin_amdgcn_readlane(e, 3)));
-      if (unit.leaves<4>(most)) unit.follow<4>(most);
+      int most = max(e, __builtin_amdgcn_mov_dpp(e, 0xB1, 0xf, 0xf, true));  // of the lane's four, which are the tile's
+      most = __builtin_amdgcn_readfirstlane(max(most, __builtin_amdgcn_mov_dpp(most, 0x4E, 0xf, 0xf, true)));
+      if (unit.leaves(most)) unit.move(most, most);
       const ValueScale v = value_scale(__builtin_ldexpf(bvs, -unit.u));
       if (lane < 4) {
         blocks[(p - tb) & 3][lane] = make_float4(bks, v.u, v.rv, bthere);
-        factors[(p - tb) & 3][lane] = make_uint2(v.m, v.n);
+        factors[(p - tb) & 3][lane] = v.m;
       }
       if (lane == 0) units[(p - tb) & 3] = unit.u;
     }
@@ -642,6 +647,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   auto bring = [&](int p, auto par) __attribute__((always_inline)) {
     constexpr int odd = decltype(par)::value;
     uint8_t *kbase = lds + odd * G::KEYS, *vbase = lds + (2 + (odd ^ 1)) * G::KEYS;
+    const uint32_t less = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, factor) * h2{(_Float16)-1152.0f, (_Float16)-1152.0f});
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
       if (none(i)) break;
@@ -656,9 +662,8 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
         *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1]);
         *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3]);
       } else {
-        const uint2 f = factors[(p - 1 - tb) & 3][pc.vt >> 4];  // (of tile p - 1, in LDS since the last step)
-        *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1], f.x, f.y);
-        *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3], f.x, f.y);
+        *(h8 *)vd = codes_h8((uint32_t)vx[i][0], (uint32_t)vx[i][1], factor, less);
+        *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3], factor, less);
       }
     }
     entries(p + 2, ent[odd]);
@@ -706,6 +711,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     constexpr std::integral_constant<int, decltype(which)::value ^ 1> other;
     const bool next = i < te && i * 64 < any_hi && i * 64 + 64 > any_lo;
     if (i < te) {
+      if constexpr (!WIDE) tile_unit[decltype(which)::value] = __builtin_amdgcn_readfirstlane(next_unit);
       bring_blocks(i + 1, other);
       bring(i + 1, other);
     }
@@ -719,9 +725,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     if (!busy) return;
     const int t0 = i * 64;
     const float4 b0 = blocks[(i - tb) & 3][c], b1 = blocks[(i - tb) & 3][2 + c];
-    const int tu = WIDE ? wide_unit[b] : __builtin_amdgcn_readfirstlane(units[(i - tb) & 3]), moved = ou - tu;
-    ou = tu;
-    if (moved) {
+    const int moved = ou - tile_unit[b];
+    ou = tile_unit[b];
+    if (D <= 128 && moved) {
       const float by = __builtin_ldexpf(1.0f, moved);
 #pragma unroll
       for (int d = 0; d < DT; ++d) O[d] *= by;
@@ -755,12 +761,14 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       mx = fmaxf(mx, m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[u], __builtin_amdgcn_fractf(lv[u])));
     }
     mx = other_half_max(mx);
-    if (__any(mx > M + kSlack)) {
+    // (heads of 256: one place for both, a second costs 6 %; smaller ones: two, 0.5 %)
+    if ((D > 128 && moved) || __any(mx > M + kSlack)) {
       const float mn = fmaxf(M, mx), alpha = exp2_fast(M - (mn == -INFINITY ? 0.0f : mn));
+      const float by = D > 128 ? __builtin_ldexpf(alpha, moved) : alpha;
       M = mn;
       L *= alpha;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) O[d] *= alpha;
+      for (int d = 0; d < DT; ++d) O[d] *= by;
     }
     const float ms = M == -INFINITY ? 0.0f : M;
     auto weights = [&](auto some) __attribute__((always_inline)) {
@@ -791,6 +799,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     bring_blocks(tb, even);
     bring(tb, even);  // (there are no values yet: those of tile tb, twice)
     __syncthreads();
+    see_blocks(tb);
     // One barrier a step: what a step brings to LDS is read in the next, and takes the
     // place of what was read in the step before.
     auto both = [&](int i, auto which) __attribute__((always_inline)) {
@@ -798,6 +807,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       products(i, which);
       __builtin_amdgcn_s_setprio(0);
       __syncthreads();
+      see_blocks(i + 1);
       if (i < te) weigh(i, which);
     };
     for (int i = tb; i <= te; i += 2) {
