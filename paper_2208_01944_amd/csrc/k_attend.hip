@@ -160,7 +160,7 @@ __device__ __forceinline__ h8 scaled(v4i raw, float f) {
 // NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
 // fourth tile of 64 tokens; the waves join in LDS, splits in attend_join_kernel.
 // Operands go from memory straight into registers, one tile ahead.  32 requests of 2047
-// to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 115 us, 5.3 TB/s (a
+// to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 117 us, 5.2 TB/s (a
 // plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 21 us.
 template <class T, int D, int NQ>
 __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
@@ -452,7 +452,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 // 4 requests, 1531 to 2048 tokens behind cached ones, 2100 to 4096 in all, 8 heads of
 // 128, group 4: 324 us, 766 TFLOP/s (a bf16 library product of 8192^3: 1240 to 1270).  A
 // wave's step of 64 tokens takes about 4000 cycles alone, 1024 of them products; the softmax
-// is 28 % of the time (234 us without), the conversion 8 % (298).
+// is 28 % of the time (232 us without), the conversion 9 % (294).
 //
 // LDS holds each matrix operand as the 1 KB that a wave reads, lane after lane, so
 // a read is a lane's own address plus a constant and meets no bank twice; the
@@ -473,7 +473,7 @@ struct TileLds {
 
 // Keeps kAhead operand reads in flight before the N products of this block: an LDS
 // read takes the time of four products, and the compiler by itself asks for one
-// operand at a time (4 requests, 2048 tokens of 4096: 451 us, 458 without).  With one more in
+// operand at a time (4 requests, 2048 tokens of 4096: 450 us, 457 without).  With one more in
 // flight the narrow pages' build for heads of 128 has no registers left for any: 153 us become
 // 167 (4 requests, 900 to 1100 tokens of 2048, pages of 32).
 constexpr int kAhead = 4;
@@ -909,7 +909,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // While the small blocks are at most 3 for each CU, their many waves over the
 // tokens end sooner than the tile kernel's long chain of steps, although each
 // block converts its codes itself: 4 requests, 8 heads, group 4, 2048 tokens, 64 /
-// 128 / 256 new ones: 30 / 40 / 72 us against 36 / 40 / 58.
+// 128 / 256 new ones: 29 / 39 / 72 us against 35 / 40 / 58.
 int block_rows(const AttendArgs &a, int cus) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
   return (rows + small - 1) / small * a.c.heads * a.b.requests <= 3 * cus ? (int)small : 128;
