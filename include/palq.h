@@ -565,6 +565,81 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
                            int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head, int32_t type,
                            float scale, int32_t causal, int32_t window);
 
+/* ------------------------------------- a generation step around the cache
+ *
+ * What stands between the products above, the cache and the next token: norms and
+ * rotation of queries and keys, attention that keeps a request's first tokens
+ * beside a window or follows a tree of drafted tokens, and the log probabilities
+ * by which tokens are chosen and drafts are checked.
+ */
+
+/* A batch's new tokens as trees, one a request (checking several drafts at
+ * once).  mask (device, 8-byte aligned): uint64 [tokens][words], words 1 to
+ * PALQ_TREE_WORDS; bit b (of word b / 64, from the lowest) of a row stands for
+ * new token b of its request (row starts[r] + b) and says whether the row sees
+ * it; a row's own bit is no different.  Bits past the request's new tokens are
+ * ignored, new tokens past 64 words are seen by none.  The position of a row is
+ * that of the request's first new token plus the number of new tokens that it
+ * sees besides itself: its depth, where bits are a token's ancestors. */
+#define PALQ_TREE_WORDS 16
+typedef struct {
+  const uint64_t *mask;
+  int32_t words;
+} palq_tree;
+
+/* The frequencies of a rotation, for any number of calls. */
+typedef struct palq_rotation palq_rotation;
+
+/* freq: HOST array of `pairs` (1 to 128) finite frequencies in radians a
+ * position; copied.  Pair i of a head is channels i and i + pairs, or 2 i and
+ * 2 i + 1 with interleaved = 1; channels from 2 pairs on do not rotate.
+ * Synchronises the context's stream.  PALQ_ERR_NOMEM.  A validate-only context
+ * returns a rotation that runs nothing. */
+palq_status palq_rotation_create(palq_ctx *ctx, const double *freq, int32_t pairs, int32_t interleaved, palq_rotation **out);
+/* Frees a rotation (waits for device work that still reads it). */
+void palq_rotation_destroy(palq_rotation *rot);
+
+/* RMS norm of every head of queries and keys, then the rotation of its pairs
+ * (a, b) by position, in fp32 and with one rounding:
+ *   y = x / sqrt(mean(x^2) + eps) * weight,  t = position * freq,
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
+ * q, k and their results: `type` (PALQ_F32, F16 or BF16) [tokens][heads]
+ * [head_dim], head_dim 64, 96, 128 or 256, strides in elements as in
+ * palq_cache_append; q_heads or k_heads 0: no such tensor.  eps 0: no norm;
+ * weights fp32 [head_dim], or NULL for ones.  rot NULL: no rotation.  Row i of
+ * request r is at position lens[r] - starts[r + 1] + i, or where `tree`
+ * (nullable) puts it; its fraction of a turn is exact to position 2^-65 and the
+ * rounding of freq, however far the position.  Of the batch, table, max_pages and
+ * max_len have no effect.  Rows past max_new stay as they are.  Results may be
+ * in place (the same pointer and strides); other overlaps of a result are
+ * refused, where tensors of different strides count as their whole ranges.
+ * Enqueues one kernel (or more where bounds are loose), and nothing else. */
+palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq_batch *batch, const palq_tree *tree, const void *q,
+                             int64_t q_row, int64_t q_head, int32_t q_heads, void *q_out, int64_t q_out_row, int64_t q_out_head,
+                             const float *q_weight, const void *k, int64_t k_row, int64_t k_head, int32_t k_heads, void *k_out,
+                             int64_t k_out_row, int64_t k_out_head, const float *k_weight, int32_t head_dim, int32_t type, float eps);
+
+/* Log probabilities of given tokens, entropy, and the most probable tokens:
+ *   l[r][i] = scale x[r][i] - ln sum_j exp(scale x[r][j])   (natural logarithm)
+ * logits x: `type` (PALQ_F32, F16 or BF16) [rows], ld elements apart, of `vocab`
+ * (up to 2^30) tokens; scale (one over a temperature): 2^-119 to 2^119.
+ *   ids int32 [rows][given] -> out fp32 [rows][given]: l of those tokens (NaN
+ *   for an id outside [0, vocab)); given may be 0
+ *   entropy fp32 [rows] (nullable): -sum_i exp(l) l
+ *   top_ids int32 [rows][top], top_out fp32 [rows][top]: the `top` (0 to
+ *   PALQ_TOP_MAX, at most vocab) largest logits in order, of equal ones the
+ *   lowest index first (-0 equals 0), and their l
+ * all device.  A token of logit -inf has l = -inf and counts 0 in the entropy; a
+ * row of nothing else has l = -inf throughout and entropy 0.  A row with NaN or
+ * +inf has NaN for every l and its entropy, and -1 for its top ids.  Sums are fp32
+ * under the row's largest logit; results do not depend on how a row is cut.
+ * Few rows are split and joined in the context's workspace, which may grow
+ * (never while a graph is captured: PALQ_ERR_NOMEM then; run the shape once
+ * before). */
+#define PALQ_TOP_MAX 64
+palq_status palq_log_probs(palq_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t vocab, int64_t ld, float scale,
+                           const int32_t *ids, int32_t given, float *out, float *entropy, int32_t top, int32_t *top_ids, float *top_out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libpalq.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["palq_api.cpp", "palq_net.cpp", "k_elementwise.hip", "k_conv_direct.hip", "k_conv_mfma.hip", "k_conv_fp.hip",
-           "palq_serve.cpp", "k_linear.hip", "k_cache.hip", "k_attend.hip"]
+           "palq_serve.cpp", "k_linear.hip", "k_cache.hip", "k_attend.hip", "k_rotate.hip", "k_score.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -1,0 +1,233 @@
+// RMS norm of every head of queries and keys, and the rotation by position, in
+// one pass:
+//   y = x / sqrt(mean(x^2) + eps) * w,
+//   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t), t = position * frequency
+// for the pairs (a, b) of a head's rotating channels.
+//
+// Angles.  A far position times a frequency loses its fraction of a turn in fp32, so
+// frequencies come as turns a position in 2^-64 of one: the product with the
+// position, modulo 2^64, is the fraction, off by at most position 2^-65 turns.  Its
+// upper 32 bits give the nearest quarter turn and a rest within an eighth, where
+// the Taylor sums of sine (to x^9) and cosine (to x^10) end below 2^-28.
+//
+// Bound by memory: each element is read and written once.  16 channels, 8 pairs, a
+// lane, so a head is 4 to 16 lanes of one wave, pairs stay in their lane and the
+// mean takes 2 to 4 steps between neighbours; a wave takes all heads of a token where
+// there are tokens enough, so that angles are formed once a token.
+#include <algorithm>
+
+#include "rotate.h"
+
+namespace palq {
+
+namespace {
+
+struct Turn { float c, s; };
+__device__ __forceinline__ Turn turn_of(uint64_t t) {
+  const int32_t v = (int32_t)(t >> 32), q = (int32_t)(((uint32_t)v + 0x20000000u) >> 30);
+  const float x = (float)(int32_t)((uint32_t)v - ((uint32_t)q << 30)) * 1.46291807926715968e-9f;  // 2 pi / 2^32
+  const float z = x * x;
+  float s = __builtin_fmaf(z, 2.75573192e-6f, -1.98412698e-4f);
+  s = __builtin_fmaf(z, s, 8.33333333e-3f);
+  s = __builtin_fmaf(z, s, -1.66666667e-1f);
+  s = __builtin_fmaf(z * s, x, x);
+  float c = __builtin_fmaf(z, -2.75573192e-7f, 2.48015873e-5f);
+  c = __builtin_fmaf(z, c, -1.38888889e-3f);
+  c = __builtin_fmaf(z, c, 4.16666667e-2f);
+  c = __builtin_fmaf(z, c, -0.5f);
+  c = __builtin_fmaf(z, c, 1.0f);
+  const float a = q & 1 ? s : c, b = q & 1 ? c : s;
+  return {(q + 1) & 2 ? -a : a, q & 2 ? -b : b};
+}
+
+template <int CTRL>
+__device__ __forceinline__ float other(float x) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+// Sum over L neighbouring lanes (4, 8 or 16).
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+  x += other<0xB1>(x);
+  x += other<0x4E>(x);
+  if constexpr (L >= 8) x += other<0x141>(x);  // (the other four of eight, reversed)
+  if constexpr (L >= 16) x += other<0x140>(x);
+  return x;
+}
+
+// Channels of a lane's pair i of 8, p the pair's index within the head.  HALVES: channel p
+// with p + pairs, eight of each in a row; NEIGHBOURS: 2 p with 2 p + 1, sixteen in a row;
+// MIXED: halves that eight does not divide, an element at a time.  Past the rotating pairs
+// all take 2 p and 2 p + 1.
+enum { HALVES, NEIGHBOURS, MIXED };
+
+template <class T>
+__device__ __forceinline__ void store8(typename T::raw *p, const float *v) {
+  store4<T>(p, v);
+  store4<T>(p + 4, v + 4);
+}
+template <>
+__device__ __forceinline__ void store8<F16>(uint16_t *p, const float *v) {
+  v4i o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = (int)((uint32_t)F16::put(v[2 * i]) | (uint32_t)F16::put(v[2 * i + 1]) << 16);
+  store_any(p, o);
+}
+template <>
+__device__ __forceinline__ void store8<BF16>(uint16_t *p, const float *v) {
+  v4i o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = (int)((uint32_t)BF16::put(v[2 * i]) | (uint32_t)BF16::put(v[2 * i + 1]) << 16);
+  store_any(p, o);
+}
+
+// 16 channels of a lane as 8 pairs: first elements, then second ones.
+template <class T, int FORM>
+struct Lane {
+  float v[16];
+  // first channels of the two runs of eight
+  static __device__ __forceinline__ void runs(int lane, int pairs, int &a, int &b) {
+    const bool rot = FORM == HALVES && 8 * lane < pairs;
+    a = rot ? 8 * lane : 16 * lane;
+    b = rot ? a + pairs : a + 8;
+  }
+  static __device__ __forceinline__ int first(int p, int pairs) { return FORM == MIXED && p < pairs ? p : 2 * p; }
+  static __device__ __forceinline__ int second(int p, int pairs) { return FORM == MIXED && p < pairs ? p + pairs : 2 * p + 1; }
+  __device__ __forceinline__ void load(const typename T::raw *x, int lane, int pairs) {
+    if constexpr (FORM == MIXED) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = T::get(x[first(8 * lane + i, pairs)]);
+        v[8 + i] = T::get(x[second(8 * lane + i, pairs)]);
+      }
+    } else {
+      int a, b;
+      runs(lane, pairs, a, b);
+      load8<T>(x + a, v);
+      load8<T>(x + b, v + 8);
+    }
+  }
+  __device__ __forceinline__ void store(typename T::raw *y, int lane, int pairs) const {
+    if constexpr (FORM == MIXED) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        y[first(8 * lane + i, pairs)] = T::put(v[i]);
+        y[second(8 * lane + i, pairs)] = T::put(v[8 + i]);
+      }
+    } else {
+      int a, b;
+      runs(lane, pairs, a, b);
+      store8<T>(y + a, v);
+      store8<T>(y + b, v + 8);
+    }
+  }
+};
+
+// One wave: `each` blocks of 64 / L heads of a token, of `parts` such shares.  Queries' blocks
+// come before the keys'.
+template <class T, int L, int FORM>
+__global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first_row, int parts, int each) {
+  constexpr int HEADS = 64 / L;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (L - 1), sub = (threadIdx.x & 63) / L;
+  const int r = blockIdx.y;
+  const Request q = request_of(a.b, r);
+  const uint32_t share = blockIdx.x * 4 + wave, rank = share / (uint32_t)parts;  // (below 2^26)
+  if (first_row + rank >= q.n) return;
+  const int t = (int)(first_row + rank), part = (int)(share - rank * parts);
+  const int64_t row = q.row0 + t;
+  int64_t pos = q.pos + (int64_t)t;
+  if (a.tree.mask) {
+    const Draft d = draft_of(a.b, r, a.tree.words);
+    pos = (int64_t)d.old + depth_of(a.tree.mask + row * a.tree.words, a.tree.words, d.n, (int)min((int64_t)d.first + t, (int64_t)1 << 30));
+  }
+  const bool there = 16 * lane < a.dim;
+  const int mine = there ? lane : 0;
+  float c[8], s[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int p = 8 * mine + i;
+    const Turn u = p < a.pairs ? turn_of((uint64_t)pos * a.phase[p]) : Turn{1.0f, 0.0f};
+    c[i] = u.c;
+    s[i] = u.s;
+  }
+  const int q_blocks = (a.heads[0] + HEADS - 1) / HEADS, blocks = q_blocks + (a.heads[1] + HEADS - 1) / HEADS;
+  const int from = part * each, to = min(from + each, blocks);
+  Lane<F32, FORM> w;
+  int have = -1;
+  typedef typename T::raw Raw;
+  const float mean = 1.0f / (float)a.dim;
+  for (int b = from; b < to; ++b) {
+    const int which = b >= q_blocks, h = (b - (which ? q_blocks : 0)) * HEADS + sub;
+    const bool live = there && h < a.heads[which];
+    const int hh = live ? h : 0;
+    Lane<T, FORM> x;
+    x.load((const Raw *)a.x[which] + row * a.x_row[which] + hh * a.x_head[which], mine, a.pairs);
+    if (a.eps != 0.0f) {
+      if (have != which && a.w[which]) w.load(a.w[which], mine, a.pairs);
+      have = which;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(x.v[i], x.v[i], sum);
+      sum = lanes_sum<L>(there ? sum : 0.0f);
+      float inv = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, mean, a.eps));
+      if (__any(sum == INFINITY)) {  // squares past fp32's range: those of x 2^-70, beside which eps is nothing
+        float less = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float z = x.v[i] * 8.470329472543003e-22f;
+          less = __builtin_fmaf(z, z, less);
+        }
+        less = lanes_sum<L>(there ? less : 0.0f);
+        if (sum == INFINITY) inv = __builtin_amdgcn_rsqf(less * mean) * 8.470329472543003e-22f;
+      }
+      if (a.w[which]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.v[i] = x.v[i] * inv * w.v[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.v[i] *= inv;
+      }
+    }
+    Lane<T, FORM> y = x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      constexpr bool near = FORM == NEIGHBOURS;
+      const int ia = near ? 2 * i : i, ib = near ? 2 * i + 1 : 8 + i;
+      if (8 * mine + i < a.pairs) {
+        y.v[ia] = __builtin_fmaf(x.v[ia], c[i], -(x.v[ib] * s[i]));
+        y.v[ib] = __builtin_fmaf(x.v[ib], c[i], x.v[ia] * s[i]);
+      }
+    }
+    if (live) y.store((Raw *)a.y[which] + row * a.y_row[which] + h * a.y_head[which], mine, a.pairs);
+  }
+}
+
+template <class T, int L>
+hipError_t launch_rotate_l(const RotateArgs &a, hipStream_t s) {
+  constexpr int HEADS = 64 / L;
+  const int blocks = (a.heads[0] + HEADS - 1) / HEADS + (a.heads[1] + HEADS - 1) / HEADS;
+  // a token's heads are shared by as many waves as it takes to have 8 on every SIMD (1024)
+  const int parts = (int)std::min<int64_t>(blocks, std::max<int64_t>(1, 8192 / std::max<int64_t>(1, a.b.tokens)));
+  const int each = (blocks + parts - 1) / parts, shares = (blocks + each - 1) / each;
+  const int64_t most = std::max<int64_t>(1, kMaxGroups * 4 / shares - 4);  // rows of a launch
+  const int64_t rows = std::min<int64_t>(a.b.max_new, a.b.tokens);
+  for (int64_t r0 = 0; r0 < rows; r0 += most) {
+    const int64_t n = std::min(rows - r0, most);
+    const dim3 g((unsigned)((n * shares + 3) / 4), (unsigned)a.b.requests);
+    if (a.interleaved || a.pairs == 0) rotate_kernel<T, L, NEIGHBOURS><<<g, 256, 0, s>>>(a, r0, shares, each);
+    else if (a.pairs % 8 == 0) rotate_kernel<T, L, HALVES><<<g, 256, 0, s>>>(a, r0, shares, each);
+    else rotate_kernel<T, L, MIXED><<<g, 256, 0, s>>>(a, r0, shares, each);
+  }
+  return hipGetLastError();
+}
+template <class T>
+hipError_t launch_rotate_t(const RotateArgs &a, hipStream_t s) {
+  return a.dim == 64 ? launch_rotate_l<T, 4>(a, s) : a.dim == 256 ? launch_rotate_l<T, 16>(a, s) : launch_rotate_l<T, 8>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_rotate(const RotateArgs &a, int type, hipStream_t s) {
+  return type == PALQ_F32 ? launch_rotate_t<F32>(a, s) : type == PALQ_F16 ? launch_rotate_t<F16>(a, s) : launch_rotate_t<BF16>(a, s);
+}
+
+}  // namespace palq

@@ -1,0 +1,395 @@
+// Log probabilities of given tokens, entropy and the k most probable tokens of a row
+// of logits x, with c = scale log2(e) and M the row's largest:
+//   S = sum_j 2^((x_j - M) c),  E = sum_j 2^((x_j - M) c) (x_j - M) c,
+//   log p_i = (x_i - M) scale - ln S,  H = ln S - ln 2 E / S.
+//
+// One pass: a wave takes a row, or a part of one, 2048 logits a step.  M runs along, for
+// each lane by itself, and moves only when a logit passes it by more than 2^8 (sums
+// then stay far inside fp32), so most steps are an exponential and two sums an
+// element; the join brings all lanes to the row's true largest, where the
+// probability of a certain token loses nothing.
+//
+// The k largest.  A logit and its index as one 64-bit key (the value in the order of
+// integers, then the index from above) have no ties, so any order of work gives the
+// same list.  A wave keeps the 64 largest keys sorted, one a lane.  A step's maxima are
+// compared with the k-th; only where one passes are single logits looked at, and
+// those that pass are collected in LDS until they are sorted (bitonic, 21 exchanges
+// between lanes, all in registers) and merged (7 more).  The first step takes its bound from the k-th
+// largest of the lanes' own maxima.  Of n logits in random order k ln(n / k) pass.
+//
+// Bound by memory, with 10 vector operations an element beside it.
+#include <algorithm>
+#include <float.h>
+
+#include "score.h"
+
+namespace palq {
+
+namespace {
+
+constexpr int kStep = 2048;    // logits of a wave's step: 32 a lane
+constexpr float kSlack = 8.0f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ------------------------------------------------------------ keys and sorted lists
+typedef uint64_t Key;  // 0: none
+
+__device__ __forceinline__ uint32_t ordered(float x) {
+  const uint32_t b = __float_as_uint(x + 0.0f);  // (-0 is 0)
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t h) {
+  return __uint_as_float(h & 0x80000000u ? h ^ 0x80000000u : ~h);
+}
+__device__ __forceinline__ Key key_of(float x, int id) { return (Key)ordered(x) << 32 | (uint32_t)~id; }
+__device__ __forceinline__ int id_of(Key k) { return (int)~(uint32_t)k; }
+
+// The value of the lane whose number differs in the bits of X.
+template <int X>
+__device__ __forceinline__ int across(int v) {
+  if constexpr (X == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xf, 0xf, true);
+  else if constexpr (X == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xf, 0xf, true);
+  else if constexpr (X == 4) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x1B, 0xf, 0xf, true), 0x141, 0xf, 0xf, true);  // 3, then 7
+  else if constexpr (X == 8) return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true), 0x140, 0xf, 0xf, true);  // 7, then 15
+  else if constexpr (X == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);  // even rows of 16 everywhere, odd ones
+    return threadIdx.x & 16 ? (int)r[0] : (int)r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return threadIdx.x & 32 ? (int)r[0] : (int)r[1];
+  }
+}
+template <int X>
+__device__ __forceinline__ Key across(Key k) {
+  return (Key)(uint32_t)across<X>((int)(k >> 32)) << 32 | (uint32_t)across<X>((int)(uint32_t)k);
+}
+template <int X>
+__device__ __forceinline__ float across(float v) { return __int_as_float(across<X>(__float_as_int(v))); }
+
+// One exchange: the larger key stays in the lower lane where `down`.
+template <int X>
+__device__ __forceinline__ Key exchange(Key k, bool down) {
+  const Key o = across<X>(k);
+  return (k > o) == (((threadIdx.x & X) == 0) == down) ? k : o;
+}
+template <int X>
+__device__ __forceinline__ Key merged(Key k, bool down) {  // a bitonic run of 2 X lanes
+  k = exchange<X>(k, down);
+  if constexpr (X > 1) k = merged<X / 2>(k, down);
+  return k;
+}
+// The wave's keys, lane 0 with the largest (down) or the smallest.
+__device__ __forceinline__ Key sorted(Key k, bool down) {
+  const int lane = threadIdx.x & 63;
+  k = merged<1>(k, ((lane & 2) == 0) == down);
+  k = merged<2>(k, ((lane & 4) == 0) == down);
+  k = merged<4>(k, ((lane & 8) == 0) == down);
+  k = merged<8>(k, ((lane & 16) == 0) == down);
+  k = merged<16>(k, ((lane & 32) == 0) == down);
+  return merged<32>(k, down);
+}
+__device__ __forceinline__ Key lane_key(Key k, int lane) {
+  return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
+
+// The `top` largest of the keys that a wave is shown.
+struct TopList {
+  Key list = 0;       // the 64 largest so far, sorted
+  Key bound = 0;      // keys at or below it are none of the top
+  int count = 0, top; // keys waiting in buf
+  Key *buf;           // 128 of LDS
+
+  __device__ __forceinline__ TopList(Key *b, int t) : top(t), buf(b) {}
+  // The k-th largest of one key of each lane bounds what the first keys have to pass.
+  __device__ __forceinline__ void start(Key most) {
+    const Key k = lane_key(sorted(most, true), top - 1);
+    bound = k ? k - 1 : 0;
+  }
+  __device__ __forceinline__ void take(Key k) {  // a key of each lane (0: none) into the list
+    k = sorted(k, false);
+    list = merged<32>(list > k ? list : k, true);
+    const Key last = lane_key(list, top - 1);
+    bound = last > bound ? last : bound;
+  }
+  __device__ __forceinline__ void show(Key k) {
+    const bool pass = k > bound;
+    const uint64_t who = __ballot(pass);
+    if (who == 0) return;
+    if (pass) buf[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0))] = k;
+    count += __popcll(who);
+    if (count >= 64) {
+      const int lane = threadIdx.x & 63;
+      __builtin_amdgcn_wave_barrier();
+      const Key now = buf[lane], rest = buf[64 + lane];
+      __builtin_amdgcn_wave_barrier();
+      count -= 64;
+      if (lane < count) buf[lane] = rest;
+      take(now);
+    }
+  }
+  __device__ __forceinline__ void settle() {
+    if (count == 0) return;
+    const int lane = threadIdx.x & 63;
+    __builtin_amdgcn_wave_barrier();
+    take(lane < count ? buf[lane] : 0);
+    __builtin_amdgcn_wave_barrier();
+    count = 0;
+  }
+};
+
+// ------------------------------------------------------------ sums
+struct Sums {
+  float m = -FLT_MAX, s = 0.0f, e = 0.0f;
+  // To a maximum m2.  (Where nothing was summed the distance may be infinite; NaN stays in s.)
+  __device__ __forceinline__ void move(float m2, float c) {
+    const float d = fmaxf((m - m2) * c, -1e30f), w = exp2_fast(d);
+    e = (e + d * s) * w;
+    s *= w;
+    m = m2;
+  }
+};
+
+// What a row's results come from: sums under its largest, and its list of keys.
+template <class T>
+__device__ __forceinline__ void finish(const ScoreArgs &a, int64_t row, const Sums &z, Key list) {
+  const int lane = threadIdx.x & 63;
+  const bool nan = z.s != z.s, none = z.s == 0.0f;
+  const float shift = none ? 0.0f : logf(z.s);
+  // (halves: the difference itself may be past fp32's range where its product is not)
+  auto logp = [&](float x) { return nan ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : (0.5f * x - 0.5f * z.m) * (2.0f * a.scale) - shift; };
+  if (a.entropy && lane == 0) a.entropy[row] = nan ? __uint_as_float(0x7fc00000u) : none ? 0.0f : fmaxf(shift - kLn2 * (z.e / z.s), 0.0f);
+  for (int i = lane; i < a.given; i += 64) {
+    const int id = a.ids[row * a.given + i];
+    a.out[row * a.given + i] = (uint32_t)id < (uint32_t)a.vocab ? logp(T::get(((const typename T::raw *)a.x)[row * a.ld + id])) : __uint_as_float(0x7fc00000u);
+  }
+  if (lane < a.top) {
+    a.top_ids[row * a.top + lane] = nan ? -1 : id_of(list);
+    a.top_out[row * a.top + lane] = logp(value_of((uint32_t)(list >> 32)));
+  }
+}
+
+__device__ __forceinline__ Sums joined(Sums z, float most, float c) {
+  z.move(most, c);
+#define PALQ_STEP(X)      \
+  z.s += across<X>(z.s);  \
+  z.e += across<X>(z.e);
+  PALQ_STEP(1) PALQ_STEP(2) PALQ_STEP(4) PALQ_STEP(8) PALQ_STEP(16) PALQ_STEP(32)
+#undef PALQ_STEP
+  return z;
+}
+__device__ __forceinline__ float wave_most(float m) {
+  m = fmaxf(m, across<1>(m));
+  m = fmaxf(m, across<2>(m));
+  m = fmaxf(m, across<4>(m));
+  m = fmaxf(m, across<8>(m));
+  m = fmaxf(m, across<16>(m));
+  return fmaxf(m, across<32>(m));
+}
+
+// A part's results in memory: {largest, S, E, 0}, then its keys.
+__device__ __forceinline__ float *part_sums(const ScoreArgs &a, int64_t unit) { return a.part + unit * 4; }
+__device__ __forceinline__ Key *part_keys(const ScoreArgs &a, int64_t units, int64_t unit) { return (Key *)(a.part + units * 4) + unit * a.top; }
+
+template <class T, bool TOP>
+__global__ __launch_bounds__(256) void score_kernel(ScoreArgs a, int64_t first_row, int64_t rows) {
+  typedef typename T::raw Raw;
+  constexpr int VEC = 16 / sizeof(Raw), U = kStep / (64 * VEC);
+  __shared__ Key bufs[TOP ? 4 : 1][128];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+  if (unit >= rows * a.splits) return;
+  const int64_t row = first_row + unit / a.splits;
+  const int split = (int)(unit % a.splits);
+  // places count from the last multiple of 16 bytes at or before the row: logit i at place from + i
+  const Raw *x = (const Raw *)a.x + row * a.ld;
+  const int from = (int)((uintptr_t)x & 15) / (int)sizeof(Raw), to = from + a.vocab;
+  x -= from;
+  const float c = a.scale * kLog2e;
+  const int last = min((to + kStep - 1) / kStep, (split + 1) * a.each);
+
+  v4i now[U], next[U];
+  auto load = [&](int step, v4i *d) __attribute__((always_inline)) {
+    const int p0 = step * kStep;
+    if (p0 >= from && p0 + kStep <= to) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) d[u] = *(const v4i *)(x + p0 + (u * 64 + lane) * VEC);
+    } else {  // the row's ends: single logits, and -inf outside
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int p = p0 + (u * 64 + lane) * VEC;
+        if (p >= from && p + VEC <= to) {
+          d[u] = *(const v4i *)(x + p);
+        } else {
+          Raw r[VEC];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) r[i] = p + i >= from && p + i < to ? x[p + i] : T::put(-INFINITY);
+          __builtin_memcpy(&d[u], r, 16);
+        }
+      }
+    }
+  };
+  auto get = [&](const v4i &d, int i) __attribute__((always_inline)) {
+    if constexpr (VEC == 4) return __int_as_float(d[i]);
+    else return T::get((uint16_t)((uint32_t)d[i >> 1] >> (i & 1) * 16));
+  };
+  Sums z;
+  float most = -INFINITY;
+  TopList best(bufs[TOP ? wave : 0], a.top);
+  int step = split * a.each;
+  if (step < last) load(step, now);
+  for (bool begun = false; step < last; ++step, begun = true) {
+    if (step + 1 < last) load(step + 1, next);
+    float mx[U], m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      mx[u] = get(now[u], 0);
+#pragma unroll
+      for (int i = 1; i < VEC; ++i) mx[u] = fmaxf(mx[u], get(now[u], i));
+      m = fmaxf(m, mx[u]);
+    }
+    most = fmaxf(most, m);
+    if (__any((m - z.m) * c > kSlack)) z.move(fmaxf(z.m, m), c);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float s = 0.0f, e = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const float t = (get(now[u], i) - z.m) * c, w = exp2_fast(t);
+        s += w;
+        e = __builtin_fmaf(w, fmaxf(t, -200.0f), e);  // (w = 0 from 2^-150 on: -inf must not meet it)
+      }
+      z.s += s;
+      z.e += e;
+    }
+    if constexpr (TOP) {
+      const int id0 = step * kStep - from;
+      if (!begun) {
+        Key k = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const int id = id0 + (u * 64 + lane) * VEC + i;
+            const Key o = (uint32_t)id < (uint32_t)a.vocab ? key_of(get(now[u], i), id) : 0;
+            k = o > k ? o : k;
+          }
+        best.start(k);
+      }
+      // A logit of the bound's value is below it if its index is larger, as all of this step's are if the first is.
+      uint32_t h = (uint32_t)(best.bound >> 32);
+      if (id_of(best.bound) >= id0) h -= h == 0x80000000u ? 2 : 1;
+      const float pass = best.bound ? value_of(h) : __uint_as_float(0x7fc00000u);
+      if (__any(!(m <= pass))) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (!__any(!(mx[u] <= pass))) continue;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const float v = get(now[u], i);
+            if (!__any(!(v <= pass))) continue;
+            const int id = id0 + (u * 64 + lane) * VEC + i;
+            best.show((uint32_t)id < (uint32_t)a.vocab ? key_of(v, id) : 0);
+          }
+        }
+        if (best.count >= 32) best.settle();
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) now[u] = next[u];
+  }
+  if constexpr (TOP) best.settle();
+  most = fmaxf(wave_most(most), -FLT_MAX);
+  z = joined(z, most, c);
+  if (a.splits == 1) {
+    finish<T>(a, row, z, best.list);
+    return;
+  }
+  if (lane == 0) *(v4f *)part_sums(a, unit) = v4f{z.m, z.s, z.e, 0.0f};
+  if (lane < a.top) part_keys(a, rows * a.splits, unit)[lane] = best.list;
+}
+
+// A wave a row: the parts under one maximum, the largest of their keys.
+template <class T, bool TOP>
+__global__ __launch_bounds__(256) void score_join_kernel(ScoreArgs a, int64_t first_row, int64_t rows) {
+  constexpr int N = 8;  // keys of a lane at a time
+  __shared__ Key bufs[TOP ? 4 : 1][128];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+  if (r >= rows) return;
+  const float c = a.scale * kLog2e;
+  TopList best(bufs[TOP ? wave : 0], a.top);
+  if constexpr (TOP) {
+    const Key *keys = part_keys(a, rows * a.splits, r * a.splits);
+    const int n = a.splits * a.top;
+    for (int k0 = 0; k0 < n; k0 += 64 * N) {
+      Key k[N], most = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int at = k0 + i * 64 + lane;
+        k[i] = at < n ? keys[at] : 0;
+      }
+      if (k0 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) most = k[i] > most ? k[i] : most;
+        best.start(most);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) best.show(k[i]);
+    }
+    best.settle();
+  }
+  Sums z;
+  float most = -FLT_MAX;
+  for (int s = lane; s < a.splits; s += 64) most = fmaxf(most, part_sums(a, r * a.splits + s)[0]);
+  most = wave_most(most);
+  for (int s = lane; s < a.splits; s += 64) {
+    const v4f p = *(const v4f *)part_sums(a, r * a.splits + s);
+    Sums o;
+    o.m = p[0];
+    o.s = p[1];
+    o.e = p[2];
+    o.move(most, c);
+    z.s += o.s;
+    z.e += o.e;
+  }
+  z.m = most;
+  z = joined(z, most, c);
+  finish<T>(a, first_row + r, z, best.list);
+}
+
+template <class T, bool TOP>
+hipError_t launch_score_t(const ScoreArgs &a, hipStream_t s) {
+  const int64_t most = kMaxGroups * 4 / a.splits;  // rows of a launch
+  for (int64_t r0 = 0; r0 < a.rows; r0 += most) {
+    const int64_t n = std::min(a.rows - r0, most);
+    score_kernel<T, TOP><<<(unsigned)((n * a.splits + 3) / 4), 256, 0, s>>>(a, r0, n);
+    if (a.splits > 1) score_join_kernel<T, TOP><<<(unsigned)((n + 3) / 4), 256, 0, s>>>(a, r0, n);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+void score_plan(ScoreArgs &a, int cus) {
+  // Parts of a row until 16 waves stand on every CU, of a step each at least.
+  const int64_t steps = ((int64_t)a.vocab + 15 + kStep - 1) / kStep, want = (int64_t)16 * cus / std::max<int64_t>(1, a.rows);
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(steps, 64), want));
+  a.each = (int32_t)((steps + parts - 1) / parts);
+  a.splits = (int32_t)((steps + a.each - 1) / a.each);
+}
+
+size_t score_work_bytes(const ScoreArgs &a) {
+  return a.splits == 1 ? 0 : (size_t)a.rows * a.splits * (16 + 8 * (size_t)a.top);
+}
+
+hipError_t launch_score(const ScoreArgs &a, int type, hipStream_t s) {
+  switch (type) {
+    case PALQ_F32: return a.top ? launch_score_t<F32, true>(a, s) : launch_score_t<F32, false>(a, s);
+    case PALQ_F16: return a.top ? launch_score_t<F16, true>(a, s) : launch_score_t<F16, false>(a, s);
+    default: return a.top ? launch_score_t<BF16, true>(a, s) : launch_score_t<BF16, false>(a, s);
+  }
+}
+
+}  // namespace palq

@@ -1,5 +1,6 @@
 // C ABI of the 8-bit transformer operators: host-side validation of every
 // call, the context's workspace, and dispatch to the kernels.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -9,6 +10,8 @@
 #include "cache.h"
 #include "linear.h"
 #include "palq_internal.h"
+#include "rotate.h"
+#include "score.h"
 
 using namespace palq;
 
@@ -21,6 +24,14 @@ struct palq_linear {
   uint8_t *mem = nullptr;
   int8_t *w = nullptr;
   float *w_scale = nullptr, *bias = nullptr;
+};
+
+// Turns a position of each rotating pair, in 2^-64 of one.
+struct palq_rotation {
+  palq_ctx *ctx = nullptr;
+  int device = -1;
+  int32_t pairs = 0, interleaved = 0;
+  uint64_t *phase = nullptr;
 };
 
 namespace {
@@ -154,6 +165,45 @@ palq_status check_written(palq_ctx *ctx, const palq_cache *c, const void *p, int
     return fail(ctx, PALQ_ERR_ARG, "output: overlaps the cache");
   return PALQ_OK;
 }
+
+// A [tokens][heads][dim] tensor with its strides.
+struct Rows {
+  const void *p;
+  int64_t row, head;
+  int32_t heads;
+};
+// Whether a row of one tensor shares an element with a row of the other.  Of tensors that interleave
+// (parts of one fused tensor) only those of the same strides are looked at row by row; others count as one range.
+bool tensors_meet(const Rows &a, const Rows &b, int64_t tokens, int32_t dim, int64_t size) {
+  if (tokens <= 0 || a.heads <= 0 || b.heads <= 0) return false;
+  auto bytes = [&](const Rows &t) { return ((tokens - 1) * t.row + (t.heads - 1) * t.head + dim) * size; };
+  if (!overlaps(a.p, bytes(a), b.p, bytes(b))) return false;
+  const int64_t apart = ((const char *)b.p - (const char *)a.p) / size;
+  if ((tokens > 1 && a.row != b.row) || (a.heads > 1 && b.heads > 1 && a.head != b.head)) return true;
+  const int64_t head = a.heads > 1 ? a.head : b.head, row = a.row;
+  // t row + h head + apart within (-dim, dim) for a t of (-tokens, tokens)
+  for (int64_t h = 1 - a.heads; h < b.heads; ++h) {
+    const int64_t off = h * head + apart;
+    if (tokens == 1 || row == 0) {
+      if (off > -dim && off < dim) return true;
+      continue;
+    }
+    for (int64_t t = -off / row - 1; t <= -off / row + 1; ++t)
+      if (t > -tokens && t < tokens && t * row + off > -dim && t * row + off < dim) return true;
+  }
+  return false;
+}
+
+// A tree of drafted tokens (nullable).
+palq_status check_tree(palq_ctx *ctx, const palq_tree *t, int64_t tokens) {
+  if (!t) return PALQ_OK;
+  if (t->words < 1) return fail(ctx, PALQ_ERR_ARG, "tree: words < 1");
+  if (t->words > PALQ_TREE_WORDS) return fail(ctx, PALQ_ERR_UNSUPPORTED, "tree: more than PALQ_TREE_WORDS words a row");
+  if (tokens > 0 && !t->mask) return fail(ctx, PALQ_ERR_ARG, "tree: null mask");
+  if (!aligned(t->mask, 8)) return fail(ctx, PALQ_ERR_ARG, "tree: mask must be 8-byte aligned");
+  return PALQ_OK;
+}
+TreeView view_of(const palq_tree *t) { return t ? TreeView{t->mask, t->words} : TreeView{nullptr, 0}; }
 
 CacheView view_of(const palq_cache *c) {
   CacheView v{c->k, c->v, c->k_scale, c->v_scale, c->pages, c->heads, c->head_dim, c->page_tokens, 0};
@@ -373,6 +423,157 @@ palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_ba
   }
   const hipError_t e = launch_attend(a, type, ctx->stream);
   return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "attention");
+}
+
+palq_status palq_rotation_create(palq_ctx *ctx, const double *freq, int32_t pairs, int32_t interleaved, palq_rotation **out) {
+  if (!ctx) return PALQ_ERR_ARG;
+  if (!out) return fail(ctx, PALQ_ERR_ARG, "rotation: null out");
+  *out = nullptr;
+  if (!freq) return fail(ctx, PALQ_ERR_ARG, "rotation: null frequencies");
+  if (pairs < 1 || pairs > 128) return fail(ctx, PALQ_ERR_ARG, "rotation: pairs outside [1, 128]");
+  if (interleaved != 0 && interleaved != 1) return fail(ctx, PALQ_ERR_ARG, "rotation: interleaved must be 0 or 1");
+  uint64_t phase[128];
+  for (int i = 0; i < pairs; ++i) {
+    if (!isfinite(freq[i])) return fail(ctx, PALQ_ERR_ARG, "rotation: a frequency is not finite");
+    // turns a position, its whole turns left out; 80-bit arithmetic, so that the rounding is below that of `freq` itself
+    long double f = (long double)freq[i] / 6.283185307179586476925286766559005768L;
+    f -= floorl(f);
+    const long double u = f * 18446744073709551616.0L;
+    phase[i] = u >= 18446744073709551615.0L ? 0 : (uint64_t)(u + 0.5L);
+  }
+  palq_rotation *r = new (std::nothrow) palq_rotation();
+  if (!r) return fail(ctx, PALQ_ERR_NOMEM, "rotation: host memory");
+  r->ctx = ctx;
+  r->device = ctx->device;
+  r->pairs = pairs;
+  r->interleaved = interleaved;
+  if (ctx->device >= 0) {
+    hipSetDevice(ctx->device);
+    if (hipMalloc((void **)&r->phase, sizeof(phase)) != hipSuccess) {
+      (void)hipGetLastError();
+      delete r;
+      return fail(ctx, PALQ_ERR_NOMEM, "rotation: device memory");
+    }
+    hipError_t e = hipMemcpyAsync(r->phase, phase, (size_t)pairs * 8, hipMemcpyHostToDevice, ctx->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(ctx->stream);
+    if (e != hipSuccess) {
+      palq_rotation_destroy(r);
+      return device_fail(ctx, e, "rotation: frequencies");
+    }
+  }
+  *out = r;
+  return PALQ_OK;
+}
+
+void palq_rotation_destroy(palq_rotation *rot) {
+  if (!rot) return;
+  if (rot->phase) {
+    hipSetDevice(rot->device);
+    hipFree(rot->phase);
+  }
+  delete rot;
+}
+
+palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq_batch *batch, const palq_tree *tree, const void *q,
+                             int64_t q_row, int64_t q_head, int32_t q_heads, void *q_out, int64_t q_out_row, int64_t q_out_head,
+                             const float *q_weight, const void *k, int64_t k_row, int64_t k_head, int32_t k_heads, void *k_out,
+                             int64_t k_out_row, int64_t k_out_head, const float *k_weight, int32_t head_dim, int32_t type, float eps) {
+  if (!ctx) return PALQ_ERR_ARG;
+  palq_status st;
+  if (rot && rot->ctx != ctx) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: rotation of another context");
+  if ((st = check_batch(ctx, batch)) || (st = check_tree(ctx, tree, batch->tokens))) return st;
+  if (!floating(type)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: type must be PALQ_F32, F16 or BF16");
+  if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256)
+    return fail(ctx, PALQ_ERR_UNSUPPORTED, "norm and rotation: head_dim not in {64,96,128,256}");
+  if (rot && 2 * rot->pairs > head_dim) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: more pairs than a head has");
+  if (q_heads < 0 || k_heads < 0 || q_heads + (int64_t)k_heads < 1) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: no heads");
+  if (q_heads > 65535 || k_heads > 65535) return fail(ctx, PALQ_ERR_UNSUPPORTED, "norm and rotation: more than 65535 heads");
+  if (!(eps == 0.0f || (eps >= FLT_MIN && eps <= FLT_MAX)))
+    return fail(ctx, PALQ_ERR_ARG, "norm and rotation: eps must be 0 (no norm) or a normal positive number");
+  if (eps == 0.0f && (q_weight || k_weight)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: weights without a norm (eps 0)");
+  const int64_t tokens = batch->tokens, size = size_of(type);
+  const Rows in[2] = {{q, q_row, q_head, q_heads}, {k, k_row, k_head, k_heads}};
+  const Rows to[2] = {{q_out, q_out_row, q_out_head, q_heads}, {k_out, k_out_row, k_out_head, k_heads}};
+  const float *weight[2] = {q_weight, k_weight};
+  for (int i = 0; i < 2; ++i) {
+    if (in[i].heads == 0) continue;
+    if ((st = check_rows(ctx, in[i].p, tokens, in[i].row, in[i].head, in[i].heads, head_dim, type)) ||
+        (st = check_rows(ctx, to[i].p, tokens, to[i].row, to[i].head, to[i].heads, head_dim, type)))
+      return st;
+    if (!aligned(weight[i], 4)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: weights must be 4-byte aligned");
+  }
+  for (int i = 0; i < 2 && tokens > 0; ++i) {
+    const Rows &o = to[i];
+    if (o.heads == 0) continue;
+    if (rows_meet(tokens, o.row, o.heads, o.head, head_dim, 0, true)) return fail(ctx, PALQ_ERR_ARG, "output: rows overlap");
+    const bool same = o.p == in[i].p && (o.row == in[i].row || tokens == 1) && (o.head == in[i].head || o.heads == 1);
+    if ((!same && tensors_meet(in[i], o, tokens, head_dim, size)) || tensors_meet(in[1 - i], o, tokens, head_dim, size) ||
+        tensors_meet(to[1 - i], o, tokens, head_dim, size))
+      return fail(ctx, PALQ_ERR_ARG, "norm and rotation: an output overlaps another tensor (or its input, not in place)");
+    const int64_t bytes = ((tokens - 1) * o.row + (o.heads - 1) * o.head + head_dim) * size;
+    for (const float *w : weight)
+      if (overlaps(w, 4 * (int64_t)head_dim, o.p, bytes)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: an output overlaps weights");
+    if (tree && overlaps(tree->mask, tokens * tree->words * 8, o.p, bytes))
+      return fail(ctx, PALQ_ERR_ARG, "norm and rotation: an output overlaps the tree");
+  }
+  if (ctx->device < 0 || batch->requests == 0 || tokens == 0 || batch->max_new == 0) return PALQ_OK;
+  hipSetDevice(ctx->device);
+  RotateArgs a{};
+  palq_cache one{};  // (no cache takes part: positions are not bounded by a table)
+  one.page_tokens = 16;
+  a.b = view_of(&one, batch);
+  a.tree = view_of(tree);
+  for (int i = 0; i < 2; ++i) {
+    a.x[i] = in[i].p;
+    a.y[i] = const_cast<void *>(to[i].p);
+    a.w[i] = weight[i];
+    a.heads[i] = in[i].heads;
+    a.x_row[i] = in[i].row;
+    a.x_head[i] = in[i].head;
+    a.y_row[i] = to[i].row;
+    a.y_head[i] = to[i].head;
+  }
+  if (rot) {
+    a.phase = rot->phase;
+    a.pairs = rot->pairs;
+    a.interleaved = rot->interleaved;
+  }
+  a.dim = head_dim;
+  a.eps = eps;
+  const hipError_t e = launch_rotate(a, type, ctx->stream);
+  return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "norm and rotation");
+}
+
+palq_status palq_log_probs(palq_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t vocab, int64_t ld, float scale,
+                           const int32_t *ids, int32_t given, float *out, float *entropy, int32_t top, int32_t *top_ids, float *top_out) {
+  if (!ctx) return PALQ_ERR_ARG;
+  if (!floating(type)) return fail(ctx, PALQ_ERR_ARG, "log probabilities: type must be PALQ_F32, F16 or BF16");
+  if (rows < 0 || vocab < 1 || ld < vocab || given < 0 || top < 0 || top > vocab) return fail(ctx, PALQ_ERR_ARG, "log probabilities: sizes");
+  if (top > PALQ_TOP_MAX) return fail(ctx, PALQ_ERR_UNSUPPORTED, "log probabilities: top above PALQ_TOP_MAX");
+  if (rows >= (int64_t)1 << 31 || vocab > 1 << 30) return fail(ctx, PALQ_ERR_UNSUPPORTED, "log probabilities: 2^31 rows or 2^30 tokens and more");
+  // (a difference of logits past fp32's range is then one of 2^9 or more in the exponent, as its -inf is)
+  if (!(scale >= ldexpf(1.0f, -119) && scale <= ldexpf(1.0f, 119))) return fail(ctx, PALQ_ERR_ARG, "log probabilities: scale outside [2^-119, 2^119]");
+  if (!sane(rows, ld) || !sane(rows, given)) return fail(ctx, PALQ_ERR_ARG, "log probabilities: tensor too large");
+  if (rows > 0 && (!logits || (given > 0 && (!ids || !out)) || (top > 0 && (!top_ids || !top_out))))
+    return fail(ctx, PALQ_ERR_ARG, "log probabilities: null pointer");
+  if (!aligned(logits, size_of(type)) || !aligned(ids, 4) || !aligned(out, 4) || !aligned(entropy, 4) || !aligned(top_ids, 4) || !aligned(top_out, 4))
+    return fail(ctx, PALQ_ERR_ARG, "log probabilities: pointer not aligned to its elements");
+  const struct { const void *p; int64_t bytes; } t[6] = {
+      {logits, extent(rows, vocab, ld, size_of(type))}, {ids, rows * given * 4}, {out, rows * given * 4},
+      {entropy, rows * 4}, {top_ids, rows * top * 4}, {top_out, rows * top * 4}};
+  for (int i = 2; i < 6; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return fail(ctx, PALQ_ERR_ARG, "log probabilities: an output overlaps another tensor");
+  if (ctx->device < 0 || rows == 0) return PALQ_OK;
+  hipSetDevice(ctx->device);
+  ScoreArgs a{logits, rows, ld, vocab, scale, ids, given, out, entropy, top, top_ids, top_out, 1, 1, nullptr};
+  score_plan(a, ctx->cus);
+  if (const size_t need = score_work_bytes(a)) {
+    a.part = (float *)workspace(ctx, need);
+    if (!a.part) return fail(ctx, PALQ_ERR_NOMEM, "log probabilities: workspace (in a capture: run the shape once before)");
+  }
+  const hipError_t e = launch_score(a, type, ctx->stream);
+  return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "log probabilities");
 }
 
 }  // extern "C"

@@ -159,4 +159,30 @@ __device__ __forceinline__ Request request_of(const BatchView &b, int r) {
   return q;
 }
 
+// The drafted tokens of a request (its new rows) as a tree: row i's bit b stands for new
+// token b, counted from starts[r].
+struct TreeView { const uint64_t *mask; int32_t words; };  // [tokens][words]; null: no tree
+struct Draft {
+  int32_t old;    // tokens before the first new one (below 0: as many new ones lie before the request)
+  int32_t n;      // new tokens that have a bit
+  int32_t first;  // index of the first row that is inside the tensors
+};
+__device__ __forceinline__ Draft draft_of(const BatchView &b, int r, int words) {
+  const int64_t s0 = b.starts[r], s1 = b.starts[r + 1], all = b.lens[r], n = s1 - s0, bits = 64 * words;
+  const int64_t old = all - n;
+  return {(int32_t)(old < -(1 << 30) ? -(1 << 30) : old > 0x7fffffff ? 0x7fffffff : old), (int32_t)(n < 0 ? 0 : n > bits ? bits : n),
+          (int32_t)(s0 < 0 ? -s0 > (1 << 30) ? 1 << 30 : -s0 : 0)};
+}
+// How many of the n new tokens a row sees besides itself (new token `self`).
+__device__ __forceinline__ int depth_of(const uint64_t *mask, int words, int n, int self) {
+  int depth = 0;
+  for (int w = 0; w < words; ++w) {
+    const int left = n - 64 * w, me = self - 64 * w;
+    uint64_t x = left >= 64 ? mask[w] : left <= 0 ? 0 : mask[w] & (((uint64_t)1 << left) - 1);
+    if (me >= 0 && me < 64) x &= ~((uint64_t)1 << me);
+    depth += __popcll(x);
+  }
+  return depth;
+}
+
 }  // namespace palq

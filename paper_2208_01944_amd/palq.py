@@ -77,6 +77,10 @@ class BatchDesc(ctypes.Structure):
                 ("tokens", c_i64), ("max_new", c_i32), ("max_len", c_i32)]
 
 
+class TreeDesc(ctypes.Structure):
+    _fields_ = [("mask", c_p), ("words", c_i32)]
+
+
 def _sig(name, res, *args):
     f = getattr(_lib, name)
     f.restype = res
@@ -134,6 +138,12 @@ _cache_append = _sig("palq_cache_append", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i
 _cache_read = _sig("palq_cache_read", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_p, c_i64, c_i64, c_i32)
 _attention = _sig("palq_attention", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_f,
                   c_i32, c_i32)
+P_TREE = ctypes.POINTER(TreeDesc)
+_rotation_create = _sig("palq_rotation_create", c_i32, c_p, ctypes.POINTER(ctypes.c_double), c_i32, c_i32, ctypes.POINTER(c_p))
+_rotation_destroy = _sig("palq_rotation_destroy", None, c_p)
+_norm_rotate = _sig("palq_norm_rotate", c_i32, c_p, c_p, P_BATCH, P_TREE, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_p, c_p, c_i64,
+                    c_i64, c_i32, c_p, c_i64, c_i64, c_p, c_i32, c_i32, c_f)
+_log_probs = _sig("palq_log_probs", c_i32, c_p, c_p, c_i32, c_i64, c_i32, c_i64, c_f, c_p, c_i32, c_p, c_p, c_i32, c_p, c_p)
 
 EXPORTS = ["palq_create", "palq_destroy", "palq_set_stream", "palq_set_conv_fp4", "palq_set_conv_bitdecomp", "palq_sync", "palq_last_error",
            "palq_version", "palq_row_bytes", "palq_act_bytes", "palq_pack", "palq_unpack",
@@ -143,7 +153,8 @@ EXPORTS = ["palq_create", "palq_destroy", "palq_set_stream", "palq_set_conv_fp4"
            "palq_avgsum", "palq_fc", "palq_net_create", "palq_net_destroy", "palq_forward",
            "palq_forward_image", "palq_net_tensor", "palq_net_ops", "palq_net_layer_kernels", "palq_net_layer_times",
            "palq_net_reset_times", "palq_quantize_rows", "palq_linear_create", "palq_linear_run", "palq_linear_destroy",
-           "palq_linear_kernels", "palq_cache_append", "palq_cache_read", "palq_attention"]
+           "palq_linear_kernels", "palq_cache_append", "palq_cache_read", "palq_attention",
+           "palq_rotation_create", "palq_rotation_destroy", "palq_norm_rotate", "palq_log_probs"]
 
 
 class PalqError(RuntimeError):
@@ -358,6 +369,95 @@ class Context:
         if st:
             self._check(st)
 
+    def norm_rotate(self, batch: Batch, q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=None, rotation=None, tree=None):
+        """palq_norm_rotate: each head of q and k [tokens, heads, head_dim] normed (eps None: not) and rotated by position
+        into q_out and k_out, which may be q and k.  tree: int64 masks [tokens, words]."""
+        tokens, _, dim = q.shape
+        kind, place = _TYPES.get(q.dtype), []
+        for x, y in ((q, q_out), (k, k_out)):
+            if (x is None) != (y is None):
+                raise PalqError(ERR_ARG, "k and k_out go together")
+            if x is None:
+                place.append((None, 0, 0, 0, None, 0, 0))
+                continue
+            xr, xh, x1 = x.stride()
+            yr, yh, y1 = y.stride()
+            if x.dtype != q.dtype or y.dtype != q.dtype or kind is None:
+                raise PalqError(ERR_ARG, "the tensors differ in type, or have no element type of the library")
+            if y.shape != x.shape or x.shape[0] != tokens or x.shape[2] != dim or x1 != 1 or y1 != 1:
+                raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim], results of their shapes, a head's channels consecutive")
+            place.append((x.data_ptr(), xr, xh, x.shape[1], y.data_ptr(), yr, yh))
+        for w in (q_weight, k_weight):
+            if w is not None:
+                _need(w, torch.float32, dim, "a weight")
+        if eps == 0:
+            raise PalqError(ERR_ARG, "eps must be above 0 (None: no norm)")
+        if rotation is not None and rotation.ctx is not self:
+            raise PalqError(ERR_ARG, "rotation of another context")
+        d = self.device
+        if d >= 0:
+            _on(self, batch.lens, *(t for t in (q, q_out, k, k_out, q_weight, k_weight) if t is not None))
+        tree = _tree(self, tree, tokens)
+        if batch.tokens != tokens:
+            batch.tokens = batch.desc.tokens = tokens
+        (qp, qr, qh, qn, qo, qor, qoh), (kp, kr, kh, kn, ko, kor, koh) = place
+        st = _norm_rotate(self.h, rotation.h if rotation is not None else None, batch.ref, tree, qp, qr, qh, qn, qo, qor, qoh, _ptr(q_weight),
+                          kp, kr, kh, kn, ko, kor, koh, _ptr(k_weight), dim, kind, 0.0 if eps is None else eps)
+        if st:
+            self._check(st)
+
+    def log_probs(self, logits, ids, out, entropy=None, top_ids=None, top=None, scale=1.0):
+        """palq_log_probs: log probabilities of ids int32 [rows, given] (or [rows]; None: none) under logits [rows, vocab] into
+        out fp32 of ids' shape, entropy fp32 [rows], and the most probable tokens into top_ids int32 and top fp32 [rows, n]."""
+        rows, vocab = logits.shape
+        kind, ld = _rows2(logits)
+        if vocab > _INT_MAX:
+            raise PalqError(ERR_UNSUPPORTED, "a row of 2^31 elements or more")
+        given = n = 0
+        if ids is not None:
+            given = 1 if ids.dim() == 1 else ids.shape[1]
+            _need(ids, torch.int32, rows * given, "ids")
+            if out is None or ids.shape[0] != rows or out.shape != ids.shape:
+                raise PalqError(ERR_ARG, "ids must have a row for each of the logits', and out their shape")
+            _need(out, torch.float32, rows * given, "out")
+        if (top_ids is None) != (top is None):
+            raise PalqError(ERR_ARG, "top_ids and top go together")
+        if top is not None:
+            n = top.shape[1]
+            _need(top_ids, torch.int32, rows * n, "top_ids")
+            _need(top, torch.float32, rows * n, "top")
+            if top.shape[0] != rows or top_ids.shape != top.shape:
+                raise PalqError(ERR_ARG, "top_ids and top must be [rows, n]")
+        if entropy is not None:
+            _need(entropy, torch.float32, rows, "entropy")
+        if self.device >= 0:
+            _on(self, logits, *(t for t in (ids, out, entropy, top_ids, top) if t is not None))
+        st = _log_probs(self.h, logits.data_ptr(), kind, rows, vocab, ld, scale, _ptr(ids), given, _ptr(out if given else None),
+                        _ptr(entropy), n, _ptr(top_ids), _ptr(top))
+        if st:
+            self._check(st)
+
+
+class Rotation:
+    """Frequencies of a rotation by position (palq_rotation_create): freq, in radians a position, one for each pair of
+    channels (i, i + pairs), or (2 i, 2 i + 1) where interleaved; copied."""
+
+    def __init__(self, ctx: Context, freq, interleaved=False):
+        f = np.ascontiguousarray(freq, dtype=np.float64)
+        if f.ndim != 1 or not 1 <= f.size <= 128:
+            raise PalqError(ERR_ARG, "freq must be 1 to 128 numbers")
+        self.ctx, self.pairs, self.interleaved = ctx, f.size, bool(interleaved)
+        h = c_p()
+        ctx._check(_rotation_create(ctx.h, f.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), f.size, int(self.interleaved),
+                                    ctypes.byref(h)))
+        self.h = h
+
+    def __del__(self):
+        h = getattr(self, "h", None)
+        if h:
+            _rotation_destroy(h)
+            self.h = None
+
 
 class Linear:
     """Weights of an 8-bit product with scales for each token and channel
@@ -475,6 +575,16 @@ def _together(*tensors):
     if any(t.get_device() != d for t in tensors):
         raise PalqError(ERR_ARG, "the tensors are on different devices")
     return d
+
+
+def _tree(ctx, t, tokens):
+    """Masks of a tree of drafted tokens, int64 [tokens, words], as the library takes them."""
+    if t is None:
+        return None
+    if t.dtype != torch.int64 or t.dim() != 2 or t.shape[0] != tokens or not t.is_contiguous():
+        raise PalqError(ERR_ARG, "tree must be contiguous int64 [tokens, words]")
+    _on(ctx, t)
+    return ctypes.byref(TreeDesc(t.data_ptr(), t.shape[1]))
 
 
 def _rows2(t):
