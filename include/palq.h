@@ -619,6 +619,24 @@ palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq
                              const float *q_weight, const void *k, int64_t k_row, int64_t k_head, int32_t k_heads, void *k_out,
                              int64_t k_out_row, int64_t k_out_head, const float *k_weight, int32_t head_dim, int32_t type, float eps);
 
+/* palq_attention (causal) where a window leaves a request's first tokens
+ * visible: a row at position p sees the tokens j <= p with j > p - window or
+ * j < sinks.  window 0: all of them, whatever sinks.  What lies between is not
+ * read.  Arguments, arithmetic, workspace and errors as palq_attention. */
+palq_status palq_attention_sinks(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *q, int64_t q_row,
+                                 int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head, int32_t type,
+                                 float scale, int32_t window, int32_t sinks);
+
+/* palq_attention of drafted tokens that form a tree, appended to the cache in
+ * any order of their rows: a row sees the tokens before the request's first new
+ * one (with a window those that palq_attention_sinks leaves at the row's position in the
+ * tree), and of the new ones those whose bit its mask has, whatever the window.
+ * A row that sees none gives 0.  Once a branch is accepted, appending its tokens
+ * again with lens shortened to it puts them in order. */
+palq_status palq_attention_tree(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const palq_tree *tree, const void *q,
+                                int64_t q_row, int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head,
+                                int32_t type, float scale, int32_t window, int32_t sinks);
+
 /* Log probabilities of given tokens, entropy, and the most probable tokens:
  *   l[r][i] = scale x[r][i] - ln sum_j exp(scale x[r][j])   (natural logarithm)
  * logits x: `type` (PALQ_F32, F16 or BF16) [rows], ld elements apart, of `vocab`

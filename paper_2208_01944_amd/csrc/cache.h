@@ -24,6 +24,8 @@ struct AttendArgs {
   int32_t block;                             // rows of a workgroup
   int32_t splits;                            // parts that a request's tokens are cut into
   float *part;                               // their results (attend_work_bytes)
+  int32_t sinks;                             // first tokens that a window keeps visible (0: none)
+  TreeView tree;                             // masks of the new tokens (null: in their order)
 };
 
 // Chooses kernel and parts (false: a row tile of all requests is no launch), and the device memory for the parts.

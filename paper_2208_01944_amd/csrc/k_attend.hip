@@ -1,7 +1,8 @@
 // Attention over the paged 8-bit cache:
 //   o_i = sum_j softmax_j(scale q_i . k_j) v_j,  k_j = code ks[block], v_j = code vs[block]
 // over the tokens j that query i sees (its own position and earlier ones, or a
-// window of them, or all).
+// window of them, or all; with a window, the request's first tokens too; of a tree of
+// drafted tokens, those whose bit its mask has).
 //
 // Scores and sums are fp32.  The codes are exact in fp16, so q is the only
 // operand that is rounded: each row is scaled by a power of two that brings its
@@ -123,6 +124,73 @@ __device__ __forceinline__ Reach reach_of(const AttendArgs &a, const Request &q,
   return s;
 }
 
+// What a row sees.  RANGE: a range.  SINKS: with the first tokens before it, of which
+// tiles come first, so that what lies between is never read.  TREE: a range (and first
+// tokens) of the tokens before the new ones, and the new ones by bits.
+enum { RANGE, SINKS, TREE };
+
+// A tree's rows go neither forward nor back, so their common bounds come from the
+// least and the largest position that a row can have.
+struct Canopy {
+  int old;            // first new token (below 0: the new ones up to there lie before the request)
+  int context;        // tokens before the new ones
+  int low, high;      // least and largest first token of a row's range
+};
+__device__ __forceinline__ Canopy canopy_of(const AttendArgs &a, const Request &q, int r) {
+  const Draft d = draft_of(a.b, r, a.tree.words);
+  Canopy c{max(d.old, -64 * PALQ_TREE_WORDS), max(0, min(d.old, q.len)), 0, 0};
+  if (a.window > 0) {
+    c.low = (int)max((int64_t)0, (int64_t)d.old - a.window + 1);
+    c.high = (int)min(max((int64_t)0, (int64_t)d.old + d.n - a.window + 1), (int64_t)0x7fffffff);  // (a row without a bit may see all n)
+  }
+  return c;
+}
+// Row t's range.
+__device__ __forceinline__ Reach branch_of(const AttendArgs &a, const Request &q, const Canopy &cp, int r, int t) {
+  Reach s{0, cp.context};
+  if (a.window > 0) {
+    const Draft d = draft_of(a.b, r, a.tree.words);
+    const int depth = depth_of(a.tree.mask + (q.row0 + t) * a.tree.words, a.tree.words, d.n, (int)min((int64_t)d.first + t, (int64_t)1 << 30));
+    s.lo = (int)min(max((int64_t)0, (int64_t)d.old + depth - a.window + 1), (int64_t)0x7fffffff);
+  }
+  return s;
+}
+// Bits b .. b + 15 of a row of masks; 0 outside its words.
+__device__ __forceinline__ uint32_t bits16(const uint64_t *mask, int words, int b) {
+  if (b <= -16 || b >= 64 * words) return 0;
+  const uint32_t *w = (const uint32_t *)mask;
+  const int i = b >> 5;
+  const uint32_t lo = i >= 0 ? w[i] : 0, hi = i + 1 < 2 * words ? w[i + 1] : 0;
+  return __builtin_amdgcn_alignbit(hi, lo, b & 31) & 0xffffu;
+}
+// The lowest n bits of 16.
+__device__ __forceinline__ uint32_t first16(int n) { return n >= 16 ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1; }
+// Which of the 16 tokens from tok on a row sees that has the range [lo, hi); of sinks, and of a tree's new tokens.
+__device__ __forceinline__ uint32_t seen16(const AttendArgs &a, const Request &q, int tok, int lo, int hi, const Canopy &cp, const uint64_t *mask) {
+  uint32_t m = (first16(hi - tok) & ~first16(lo - tok)) | first16(min(a.sinks, hi) - tok);
+  if (mask && tok + 16 > cp.old) m |= bits16(mask, a.tree.words, tok - cp.old) & first16(q.len - tok);
+  return m;
+}
+
+// The tiles of 64 tokens of rows that see [lo, hi), by number; SINKS, TREE: the first tokens'
+// tiles come before the others, so a tile's number is not its place.
+template <int SEES>
+struct Tiles {
+  int first, count, sink = 0, gap = 0;
+  __device__ __forceinline__ Tiles(const AttendArgs &a, int lo, int hi) {
+    const int tile0 = lo >> 6, n = hi > lo ? ((hi + 63) >> 6) - tile0 : 0;
+    first = tile0;
+    count = n;
+    if constexpr (SEES != RANGE) {
+      sink = min((int)(((int64_t)min(a.sinks, hi) + 63) >> 6), tile0);
+      gap = tile0 - sink;
+      first = 0;
+      count = sink + n;
+    }
+  }
+  __device__ __forceinline__ int at(int i) const { return SEES == RANGE || i < sink ? i : i + gap; }
+};
+
 // The power of two that brings a row's largest magnitude (its bits) to [2^14, 2^15),
 // and its inverse.  A row with inf or NaN: 0, so that inf 0 = NaN reaches all of
 // its scores.
@@ -162,7 +230,7 @@ __device__ __forceinline__ h8 scaled(v4i raw, float f) {
 // Operands go from memory straight into registers, one tile ahead.  32 requests of 2047
 // to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 117 us, 5.2 TB/s (a
 // plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 21 us.
-template <class T, int D, int NQ>
+template <class T, int D, int NQ, int SEES>
 __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
   constexpr int CH = D % 64 == 0 ? 16 : 8;  // consecutive channels of a key that a lane loads at once
@@ -179,23 +247,32 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   const int last = min(rows, first + NQ * 16) - 1;
 
   // tokens that any of the tile's rows sees, in tiles of 64
-  const Reach rf = reach_of(a, q, first / a.group), rl = reach_of(a, q, last / a.group);
+  Reach rf = reach_of(a, q, first / a.group), rl = reach_of(a, q, last / a.group);
+  Canopy cp{};
+  if constexpr (SEES == TREE) {
+    cp = canopy_of(a, q, r);
+    rf = {cp.low, cp.context};
+    rl = {cp.high, q.len};
+  }
   const int lo = rf.lo, hi = rl.hi;
-  const int tile0 = lo >> 6, ntiles = hi > lo ? ((hi + 63) >> 6) - tile0 : 0;
+  const Tiles<SEES> tiles(a, lo, hi);
+  const int tile0 = tiles.first, ntiles = tiles.count;
   const int per = (ntiles + a.splits - 1) / a.splits;
   const int tb = tile0 + min(ntiles, split * per), te = tile0 + min(ntiles, (split + 1) * per);
 
   // the rows' elements are on their way while the tokens' pages are looked up
   v4i raw[NQ][KS];
   int rlo[NQ], rhi[NQ];
+  const uint64_t *mask[SEES == TREE ? NQ : 1];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int row = first + n * 16 + col;
     const bool live = row < rows;
     const int t = live ? row / a.group : 0, g = live ? row - t * a.group : 0;
-    const Reach s = reach_of(a, q, t);
+    const Reach s = SEES == TREE ? branch_of(a, q, cp, r, t) : reach_of(a, q, t);
     rlo[n] = s.lo;
     rhi[n] = live ? s.hi : 0;
+    if constexpr (SEES == TREE) mask[n] = live ? a.tree.mask + (q.row0 + t) * a.tree.words : nullptr;
     // this lane's channels of row lane % 16 (of the first row past the last): of every
     // 64 (32 where 64 do not divide the head) the 16 (8) from 16 c (8 c) on, as the keys'
     const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * CH;
@@ -226,9 +303,9 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   uint32_t kx[4][D / 16];
   v4i vx[DT];
   auto load_k = [&](int tile) __attribute__((always_inline)) {
-    const int kt = tile * 64 + kc, vt = tile * 64 + vc;
+    const int kt = tiles.at(tile) * 64 + kc, vt = tiles.at(tile) * 64 + vc;
     const bool kok = ((uint32_t)kpage < (uint32_t)cv.pages) & (kt < hi);
-    vthere = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi) & (vt + 16 > lo);
+    vthere = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi) & ((vt + 16 > lo) | (SEES != RANGE && vt < a.sinks));
     const int8_t *kb = cv.k + (((int64_t)(kok ? kpage : 0) * heads + h) * cv.page + (kt & pm) + (col & 3)) * D + c * CH;
     const int64_t sc = (int64_t)(vthere ? vpage : 0) * heads + h;
     ks = cv.ks[sc];
@@ -256,17 +333,17 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   // the next keys wait for the entries, so these come first (into the registers that
   // the values' address has just left)
   auto load_v = [&](int tile) __attribute__((always_inline)) {
-    const int vt = tile * 64 + vc;
+    const int vt = tiles.at(tile) * 64 + vc;
     const bool ok = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
     const int8_t *vb = cv.v + (((int64_t)(ok ? vpage : 0) * heads + h) * D + col) * cv.page + (vt & pm);
-    kpage = entry((tile + 4) * 64 + kc);
-    vpage = entry((tile + 4) * 64 + vc);
+    kpage = entry(tiles.at(tile + 4) * 64 + kc);
+    vpage = entry(tiles.at(tile + 4) * 64 + vc);
 #pragma unroll
     for (int d = 0; d < DT; ++d) vx[d] = *(const v4i *)(vb + d * 16 * cv.page);
   };
   if (tb + wave < te) {
-    kpage = entry((tb + wave) * 64 + kc);
-    vpage = entry((tb + wave) * 64 + vc);
+    kpage = entry(tiles.at(tb + wave) * 64 + kc);
+    vpage = entry(tiles.at(tb + wave) * 64 + vc);
     load_k(tb + wave);
     load_v(tb + wave);
   }
@@ -295,7 +372,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   }
   auto step = [&](int tile, auto last) __attribute__((always_inline)) {
     constexpr bool more = !decltype(last)::value;
-    const int vt = tile * 64 + vc;
+    const int t0 = tiles.at(tile) * 64, vt = t0 + vc;
     const bool there = vthere;
     const float kst = ks, vst = vs;
     // (no scale of the tile from 2^5 on, one from 2^-4 on: the unit stays)
@@ -330,18 +407,20 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     // Tokens that all rows see need no masks (columns past the last row are not stored).
     // 8 requests of 17 to 131 rows, heads of 64: 18.5 us, 21.5 with masks always.  The wider
     // builds keep them: two paths took 256 registers and scratch (heads of 128, 32 rows).
-    const bool whole = D * NQ <= 128 && __all(there) && tile * 64 >= rl.lo && tile * 64 + 64 <= rf.hi;
+    const bool whole = D * NQ <= 128 && __all(there) && t0 >= rl.lo && t0 + 64 <= rf.hi;
     auto weigh = [&](int n, auto masks) __attribute__((always_inline)) {
       constexpr bool some = decltype(masks)::value;
       const float fk = f[n] * kst;
       float mx = -INFINITY;
+      uint32_t seen = 0;
+      if constexpr (some && SEES != RANGE) seen = there ? seen16(a, q, vt, rlo[n], rhi[n], cp, SEES == TREE ? mask[n] : nullptr) : 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (some) {
             const int tok = vt + 4 * j + i;
-            const bool sees = there & (tok >= rlo[n]) & (tok < rhi[n]);
+            const bool sees = SEES == RANGE ? there & (tok >= rlo[n]) & (tok < rhi[n]) : seen >> (4 * j + i) & 1;
             S[n][j][i] = sees ? __builtin_fmaf(S[n][j][i], fk, u) : -INFINITY;
           }
           mx = fmaxf(mx, S[n][j][i]);
@@ -488,7 +567,7 @@ __device__ __forceinline__ void ahead() {
   __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
 
-template <class T, int D, bool WIDE>
+template <class T, int D, bool WIDE, int SEES>
 __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(AttendArgs a, int first_tile, int row_tiles) {
   typedef TileLds<D> G;
   constexpr int ROWS = 128, KS = D / 16, DT = D / 32, PP = (4 * D + kTileThreads - 1) / kTileThreads;
@@ -507,9 +586,16 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   const int rows = q.n * a.group, first = rt * ROWS;
   if (first >= rows) return;
   const int last = min(rows, first + ROWS) - 1;
-  const Reach rf = reach_of(a, q, first / a.group), rl = reach_of(a, q, last / a.group);
+  Reach rf = reach_of(a, q, first / a.group), rl = reach_of(a, q, last / a.group);
+  Canopy cp{};
+  if constexpr (SEES == TREE) {
+    cp = canopy_of(a, q, r);
+    rf = {cp.low, cp.context};
+    rl = {cp.high, q.len};
+  }
   const int hi = rl.hi;
-  const int tile0 = rf.lo >> 6, ntiles = hi > rf.lo ? ((hi + 63) >> 6) - tile0 : 0;
+  const Tiles<SEES> tiles(a, rf.lo, hi);
+  const int tile0 = tiles.first, ntiles = tiles.count;
   const int per = (ntiles + a.splits - 1) / a.splits;
   const int tb = tile0 + min(ntiles, split * per), te = tile0 + min(ntiles, (split + 1) * per);
 
@@ -517,11 +603,12 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   const int row = first + wave * 32 + col;
   const bool live = row < rows;
   const int t = live ? row / a.group : 0, hq = h * a.group + (live ? row - t * a.group : 0);
-  const Reach mine = reach_of(a, q, t);
+  const Reach mine = SEES == TREE ? branch_of(a, q, cp, r, t) : reach_of(a, q, t);
   const int rlo = mine.lo, rhi = live ? mine.hi : 0;
+  const uint64_t *mask = SEES == TREE && live ? a.tree.mask + (q.row0 + t) * a.tree.words : nullptr;
   // tokens that all of the wave's rows see, and that any sees
   const int w0 = first + wave * 32, w1 = min(w0 + 31, last);
-  const Reach wf = reach_of(a, q, min(w0, last) / a.group), wl = reach_of(a, q, w1 / a.group);
+  const Reach wf = SEES == TREE ? rf : reach_of(a, q, min(w0, last) / a.group), wl = SEES == TREE ? rl : reach_of(a, q, w1 / a.group);
   const int all_lo = wl.lo, all_hi = w0 + 31 <= last ? wf.hi : 0, any_lo = wf.lo, any_hi = w0 <= last ? wl.hi : 0;
 
   h8 Q[KS];
@@ -564,19 +651,19 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   auto entries = [&](int p, Entries &e) __attribute__((always_inline)) {
     if constexpr (WIDE) {
       const ScalarInts st = (ScalarInts)(uintptr_t)table;
-      e.k[0] = e.b = st[__builtin_amdgcn_readfirstlane((uint32_t)min(p * 64, hi - 1) >> cv.shift)];
-      e.v[0] = st[__builtin_amdgcn_readfirstlane((uint32_t)min(max(p - 1, tb) * 64, hi - 1) >> cv.shift)];
+      e.k[0] = e.b = st[__builtin_amdgcn_readfirstlane((uint32_t)min(tiles.at(p) * 64, hi - 1) >> cv.shift)];
+      e.v[0] = st[__builtin_amdgcn_readfirstlane((uint32_t)min(tiles.at(max(p - 1, tb)) * 64, hi - 1) >> cv.shift)];
       return;
     }
 #pragma unroll
     for (int i = 0; i < PP; ++i) {
-      e.k[i] = entry(p * 64 + piece(i).tok);
-      e.v[i] = entry(max(p - 1, tb) * 64 + piece(i).vt);
+      e.k[i] = entry(tiles.at(p) * 64 + piece(i).tok);
+      e.v[i] = entry(tiles.at(max(p - 1, tb)) * 64 + piece(i).vt);
     }
-    e.b = entry(p * 64 + (threadIdx.x & 3) * 16);
+    e.b = entry(tiles.at(p) * 64 + (threadIdx.x & 3) * 16);
   };
   auto load = [&](int p, const Entries &e) __attribute__((always_inline)) {
-    const int ktile = p * 64 & pm, vtile = max(p - 1, tb) * 64 & pm;  // of a page that is wider than a tile
+    const int ktile = tiles.at(p) * 64 & pm, vtile = tiles.at(max(p - 1, tb)) * 64 & pm;  // of a page that is wider than a tile
     if constexpr (WIDE) {
       const int kp = __builtin_amdgcn_readfirstlane(valid(e.k[0]) ? e.k[0] : 0), vp = __builtin_amdgcn_readfirstlane(valid(e.v[0]) ? e.v[0] : 0);
       const int8_t *kt = kh + (uint64_t)kp * page_bytes * D, *vt = vh + (uint64_t)vp * page_bytes * D;
@@ -600,7 +687,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       kx[i] = *(const v4i *)(kh + kp + tile_key_at(pc, ktile, pm, D));
       vx[i] = *(const v4i *)(vh + vp + tile_value_at(pc, vtile, pm, cv.shift));
     }
-    const bool page = valid(e.b), reached = p * 64 + (int)(threadIdx.x & 3) * 16 + 16 > rf.lo;  // (what no row sees sets no unit)
+    const bool page = valid(e.b);
+    const int chunk = tiles.at(p) * 64 + (int)(threadIdx.x & 3) * 16;  // (what no row sees sets no unit)
+    const bool reached = (chunk + 16 > rf.lo) | (SEES != RANGE && chunk < a.sinks);
     const int64_t at = (int64_t)(page ? e.b : 0) * heads + h;
     bks = cv.ks[at];
     bvs = cv.vs[at];
@@ -709,7 +798,8 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   // the first of tile i
   auto products = [&](int i, auto which) __attribute__((always_inline)) {
     constexpr std::integral_constant<int, decltype(which)::value ^ 1> other;
-    const bool next = i < te && i * 64 < any_hi && i * 64 + 64 > any_lo;
+    const int t0 = tiles.at(i) * 64;
+    const bool next = i < te && t0 < any_hi && (t0 + 64 > any_lo || (SEES != RANGE && t0 < a.sinks));
     if (i < te) {
       if constexpr (!WIDE) tile_unit[decltype(which)::value] = __builtin_amdgcn_readfirstlane(next_unit);
       bring_blocks(i + 1, other);
@@ -723,7 +813,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   auto weigh = [&](int i, auto which) __attribute__((always_inline)) {
     constexpr int b = decltype(which)::value;
     if (!busy) return;
-    const int t0 = i * 64;
+    const int t0 = tiles.at(i) * 64;
     const float4 b0 = blocks[(i - tb) & 3][c], b1 = blocks[(i - tb) & 3][2 + c];
     const int moved = ou - tile_unit[b];
     ou = tile_unit[b];
@@ -739,11 +829,12 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const bool ok = (u ? b1.w : b0.w) != 0.0f;
+        if constexpr (SEES != RANGE) off |= (ok ? ~seen16(a, q, t0 + u * 32 + c * 16, rlo, rhi, cp, mask) & 0xffffu : 0xffffu) << (u * 16);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int tok = t0 + u * 32 + c * 16 + j;
-          const bool sees = ok & (tok >= rlo) & (tok < rhi);
-          off |= sees ? 0u : 1u << (u * 16 + j);
+          const bool sees = SEES == RANGE ? ok & (tok >= rlo) & (tok < rhi) : !(off >> (u * 16 + j) & 1u);
+          if constexpr (SEES == RANGE) off |= sees ? 0u : 1u << (u * 16 + j);
           S[u][j] = sees ? S[u][j] : -INFINITY;
         }
       }
@@ -915,7 +1006,7 @@ int block_rows(const AttendArgs &a, int cus) {
   return (rows + small - 1) / small * a.c.heads * a.b.requests <= 3 * cus ? (int)small : 128;
 }
 
-template <class T, int D>
+template <class T, int D, int SEES>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
   if (a.block == 128) {
@@ -924,13 +1015,13 @@ hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
     for (int64_t left = rt; left > 0; left -= most) {
       const int64_t n = std::min(left, most), t0 = left - n;
       const unsigned flat = (unsigned)(n * each);
-      if (a.c.page >= 64) attend_tile_kernel<T, D, true><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
-      else attend_tile_kernel<T, D, false><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
+      if (a.c.page >= 64) attend_tile_kernel<T, D, true, SEES><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
+      else attend_tile_kernel<T, D, false, SEES><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
     }
   } else {
     const dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
-    if (a.block == 16) attend_rows_kernel<T, D, 1><<<g, 256, 0, s>>>(a);
-    else if constexpr (D < 256) attend_rows_kernel<T, D, 2><<<g, 256, 0, s>>>(a);
+    if (a.block == 16) attend_rows_kernel<T, D, 1, SEES><<<g, 256, 0, s>>>(a);
+    else if constexpr (D < 256) attend_rows_kernel<T, D, 2, SEES><<<g, 256, 0, s>>>(a);
   }
   if (a.splits > 1) {
     const int64_t per = 256 / (D / 4), n = (int64_t)a.b.max_new * a.c.heads * a.group;
@@ -939,14 +1030,18 @@ hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <class T>
+template <class T, int SEES>
 hipError_t launch_attend_t(const AttendArgs &a, hipStream_t s) {
   switch (a.c.dim) {
-    case 64: return launch_attend_d<T, 64>(a, s);
-    case 96: return launch_attend_d<T, 96>(a, s);
-    case 128: return launch_attend_d<T, 128>(a, s);
-    default: return launch_attend_d<T, 256>(a, s);
+    case 64: return launch_attend_d<T, 64, SEES>(a, s);
+    case 96: return launch_attend_d<T, 96, SEES>(a, s);
+    case 128: return launch_attend_d<T, 128, SEES>(a, s);
+    default: return launch_attend_d<T, 256, SEES>(a, s);
   }
+}
+template <class T>
+hipError_t launch_attend_s(const AttendArgs &a, hipStream_t s) {
+  return a.tree.mask ? launch_attend_t<T, TREE>(a, s) : a.sinks ? launch_attend_t<T, SINKS>(a, s) : launch_attend_t<T, RANGE>(a, s);
 }
 
 }  // namespace
@@ -959,7 +1054,10 @@ bool attend_plan(AttendArgs &a, int cus) {
   // rows: its waves hold twice the accumulators; 4 requests, 5 tokens, window 8191: 24 us
   // in 8 parts, 26 in 16).  A part has two tiles or more for every wave, and what is
   // done in four is not cut at all: joining costs as much.
-  const int64_t most = a.b.max_len <= 1024 ? 1 : (a.b.max_len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
+  // (of sinks and trees the tokens that a window leaves)
+  const bool some = (a.sinks || a.tree.mask) && a.window > 0;
+  const int64_t len = some ? std::min<int64_t>(a.b.max_len, (int64_t)a.window + a.b.max_new + a.sinks) : a.b.max_len;
+  const int64_t most = len <= 1024 ? 1 : (len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), want / base));
   return (int64_t)a.splits * a.c.heads * a.b.requests <= kMaxGroups;
 }
@@ -970,7 +1068,7 @@ size_t attend_work_bytes(const AttendArgs &a) {
 }
 
 hipError_t launch_attend(const AttendArgs &a, int type, hipStream_t s) {
-  return type == PALQ_F16 ? launch_attend_t<F16>(a, s) : launch_attend_t<BF16>(a, s);
+  return type == PALQ_F16 ? launch_attend_s<F16>(a, s) : launch_attend_s<BF16>(a, s);
 }
 
 }  // namespace palq

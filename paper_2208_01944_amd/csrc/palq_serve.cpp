@@ -216,6 +216,47 @@ BatchView view_of(const palq_cache *c, const palq_batch *b) {
                    (int32_t)std::min(b->tokens, (int64_t)0x7fffffff), (int32_t)limit};
 }
 
+// The attention calls; tree nullable, sinks 0 or more.
+palq_status attend(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const palq_tree *tree, const void *q, int64_t q_row,
+                   int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head, int32_t type, float scale,
+                   int32_t causal, int32_t window, int32_t sinks) {
+  if (!ctx) return PALQ_ERR_ARG;
+  palq_status st;
+  if ((st = check_cache(ctx, cache)) || (st = check_batch(ctx, batch)) || (st = check_tree(ctx, tree, batch->tokens))) return st;
+  if (type != PALQ_F16 && type != PALQ_BF16) return fail(ctx, PALQ_ERR_ARG, "attention: type must be PALQ_F16 or PALQ_BF16");
+  if (q_heads < 1 || q_heads % cache->heads) return fail(ctx, PALQ_ERR_ARG, "attention: q_heads is no multiple of the cache's heads");
+  if ((st = check_rows(ctx, q, batch->tokens, q_row, q_head, q_heads, cache->head_dim, type)) ||
+      (st = check_rows(ctx, out, batch->tokens, out_row, out_head, q_heads, cache->head_dim, type)))
+    return st;
+  if (!isfinite(scale)) return fail(ctx, PALQ_ERR_ARG, "attention: scale must be finite");
+  if ((causal != 0 && causal != 1) || window < 0) return fail(ctx, PALQ_ERR_ARG, "attention: causal must be 0 or 1, window >= 0");
+  if (sinks < 0) return fail(ctx, PALQ_ERR_ARG, "attention: sinks must be 0 or more");
+  if (window > 0 && !causal) return fail(ctx, PALQ_ERR_ARG, "attention: a window needs causal = 1");
+  const int32_t group = q_heads / cache->heads;
+  if ((int64_t)batch->max_new * group >= (int64_t)1 << 30)
+    return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^30 or more rows of a cache head");
+  auto bytes = [&](int64_t row, int64_t head) {
+    return batch->tokens <= 0 ? 0 : ((batch->tokens - 1) * row + (q_heads - 1) * head + cache->head_dim) * size_of(type);
+  };
+  if (overlaps(q, bytes(q_row, q_head), out, bytes(out_row, out_head)))
+    return fail(ctx, PALQ_ERR_ARG, "attention: out overlaps q");
+  if (tree && overlaps(tree->mask, batch->tokens * tree->words * 8, out, bytes(out_row, out_head)))
+    return fail(ctx, PALQ_ERR_ARG, "attention: out overlaps the tree");
+  if ((st = check_written(ctx, cache, out, batch->tokens, out_row, out_head, q_heads, type))) return st;
+  if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0) return PALQ_OK;
+  hipSetDevice(ctx->device);
+  AttendArgs a{view_of(cache), view_of(cache, batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
+               group, causal, window, scale, 0, 1, nullptr, window > 0 ? sinks : 0, view_of(tree)};
+  if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
+  if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^24 or more pairs of a request and a cache head");
+  if (const size_t need = attend_work_bytes(a)) {
+    a.part = (float *)workspace(ctx, need);
+    if (!a.part) return fail(ctx, PALQ_ERR_NOMEM, "attention: workspace (in a capture: run the shape once before)");
+  }
+  const hipError_t e = launch_attend(a, type, ctx->stream);
+  return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "attention");
+}
+
 }  // namespace
 
 extern "C" {
@@ -391,38 +432,20 @@ palq_status palq_cache_read(palq_ctx *ctx, const palq_cache *cache, const palq_b
 palq_status palq_attention(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *q, int64_t q_row,
                            int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head, int32_t type,
                            float scale, int32_t causal, int32_t window) {
-  if (!ctx) return PALQ_ERR_ARG;
-  palq_status st;
-  if ((st = check_cache(ctx, cache)) || (st = check_batch(ctx, batch))) return st;
-  if (type != PALQ_F16 && type != PALQ_BF16) return fail(ctx, PALQ_ERR_ARG, "attention: type must be PALQ_F16 or PALQ_BF16");
-  if (q_heads < 1 || q_heads % cache->heads) return fail(ctx, PALQ_ERR_ARG, "attention: q_heads is no multiple of the cache's heads");
-  if ((st = check_rows(ctx, q, batch->tokens, q_row, q_head, q_heads, cache->head_dim, type)) ||
-      (st = check_rows(ctx, out, batch->tokens, out_row, out_head, q_heads, cache->head_dim, type)))
-    return st;
-  if (!isfinite(scale)) return fail(ctx, PALQ_ERR_ARG, "attention: scale must be finite");
-  if ((causal != 0 && causal != 1) || window < 0) return fail(ctx, PALQ_ERR_ARG, "attention: causal must be 0 or 1, window >= 0");
-  if (window > 0 && !causal) return fail(ctx, PALQ_ERR_ARG, "attention: a window needs causal = 1");
-  const int32_t group = q_heads / cache->heads;
-  if ((int64_t)batch->max_new * group >= (int64_t)1 << 30)
-    return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^30 or more rows of a cache head");
-  auto bytes = [&](int64_t row, int64_t head) {
-    return batch->tokens <= 0 ? 0 : ((batch->tokens - 1) * row + (q_heads - 1) * head + cache->head_dim) * size_of(type);
-  };
-  if (overlaps(q, bytes(q_row, q_head), out, bytes(out_row, out_head)))
-    return fail(ctx, PALQ_ERR_ARG, "attention: out overlaps q");
-  if ((st = check_written(ctx, cache, out, batch->tokens, out_row, out_head, q_heads, type))) return st;
-  if (ctx->device < 0 || batch->requests == 0 || batch->tokens == 0 || batch->max_new == 0) return PALQ_OK;
-  hipSetDevice(ctx->device);
-  AttendArgs a{view_of(cache), view_of(cache, batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
-               group, causal, window, scale, 0, 1, nullptr};
-  if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
-  if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^24 or more pairs of a request and a cache head");
-  if (const size_t need = attend_work_bytes(a)) {
-    a.part = (float *)workspace(ctx, need);
-    if (!a.part) return fail(ctx, PALQ_ERR_NOMEM, "attention: workspace (in a capture: run the shape once before)");
-  }
-  const hipError_t e = launch_attend(a, type, ctx->stream);
-  return e == hipSuccess ? PALQ_OK : device_fail(ctx, e, "attention");
+  return attend(ctx, cache, batch, nullptr, q, q_row, q_head, q_heads, out, out_row, out_head, type, scale, causal, window, 0);
+}
+
+palq_status palq_attention_sinks(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const void *q, int64_t q_row,
+                                 int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head, int32_t type,
+                                 float scale, int32_t window, int32_t sinks) {
+  return attend(ctx, cache, batch, nullptr, q, q_row, q_head, q_heads, out, out_row, out_head, type, scale, 1, window, sinks);
+}
+
+palq_status palq_attention_tree(palq_ctx *ctx, const palq_cache *cache, const palq_batch *batch, const palq_tree *tree, const void *q,
+                                int64_t q_row, int64_t q_head, int32_t q_heads, void *out, int64_t out_row, int64_t out_head,
+                                int32_t type, float scale, int32_t window, int32_t sinks) {
+  if (ctx && !tree) return fail(ctx, PALQ_ERR_ARG, "attention: null tree");
+  return attend(ctx, cache, batch, tree, q, q_row, q_head, q_heads, out, out_row, out_head, type, scale, 1, window, sinks);
 }
 
 palq_status palq_rotation_create(palq_ctx *ctx, const double *freq, int32_t pairs, int32_t interleaved, palq_rotation **out) {

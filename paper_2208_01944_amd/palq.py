@@ -143,6 +143,10 @@ _rotation_create = _sig("palq_rotation_create", c_i32, c_p, ctypes.POINTER(ctype
 _rotation_destroy = _sig("palq_rotation_destroy", None, c_p)
 _norm_rotate = _sig("palq_norm_rotate", c_i32, c_p, c_p, P_BATCH, P_TREE, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_p, c_p, c_i64,
                     c_i64, c_i32, c_p, c_i64, c_i64, c_p, c_i32, c_i32, c_f)
+_attention_sinks = _sig("palq_attention_sinks", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_f,
+                        c_i32, c_i32)
+_attention_tree = _sig("palq_attention_tree", c_i32, c_p, P_CACHE, P_BATCH, P_TREE, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32,
+                       c_f, c_i32, c_i32)
 _log_probs = _sig("palq_log_probs", c_i32, c_p, c_p, c_i32, c_i64, c_i32, c_i64, c_f, c_p, c_i32, c_p, c_p, c_i32, c_p, c_p)
 
 EXPORTS = ["palq_create", "palq_destroy", "palq_set_stream", "palq_set_conv_fp4", "palq_set_conv_bitdecomp", "palq_sync", "palq_last_error",
@@ -154,7 +158,8 @@ EXPORTS = ["palq_create", "palq_destroy", "palq_set_stream", "palq_set_conv_fp4"
            "palq_forward_image", "palq_net_tensor", "palq_net_ops", "palq_net_layer_kernels", "palq_net_layer_times",
            "palq_net_reset_times", "palq_quantize_rows", "palq_linear_create", "palq_linear_run", "palq_linear_destroy",
            "palq_linear_kernels", "palq_cache_append", "palq_cache_read", "palq_attention",
-           "palq_rotation_create", "palq_rotation_destroy", "palq_norm_rotate", "palq_log_probs"]
+           "palq_rotation_create", "palq_rotation_destroy", "palq_norm_rotate", "palq_attention_sinks",
+           "palq_attention_tree", "palq_log_probs"]
 
 
 class PalqError(RuntimeError):
@@ -359,11 +364,25 @@ class Context:
         if st:
             self._check(st)
 
-    def attention(self, cache: Cache, q, out, batch: Batch, scale, causal=True, window=0):
-        """palq_attention: q, out [tokens, q_heads, head_dim]."""
+    def attention(self, cache: Cache, q, out, batch: Batch, scale, causal=True, window=0, sinks=0, tree=None):
+        """palq_attention: q, out [tokens, q_heads, head_dim].  sinks: first tokens that a window leaves visible
+        (palq_attention_sinks); tree: int64 masks [tokens, words] of drafted tokens (palq_attention_tree)."""
         t, qr, qh, orow, oh = _pair3(self, q, out, batch, cache, True)
         if window < 0:
             raise PalqError(ERR_ARG, "window must be 0 or more")
+        if sinks or tree is not None:
+            if sinks < 0 or not causal:
+                raise PalqError(ERR_ARG, "sinks must be 0 or more; sinks and trees are causal")
+            window, sinks = min(window, _INT_MAX), min(sinks, _INT_MAX)
+            if tree is None:
+                st = _attention_sinks(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, t, scale,
+                                      window, sinks)
+            else:
+                st = _attention_tree(self.h, cache.ref, batch.ref, _tree(self, tree, q.shape[0]), q.data_ptr(), qr, qh, q.shape[1],
+                                     out.data_ptr(), orow, oh, t, scale, window, sinks)
+            if st:
+                self._check(st)
+            return
         st = _attention(self.h, cache.ref, batch.ref, q.data_ptr(), qr, qh, q.shape[1], out.data_ptr(), orow, oh, t, scale, causal,
                         min(window, _INT_MAX))
         if st:
