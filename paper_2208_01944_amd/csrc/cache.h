@@ -26,6 +26,9 @@ struct AttendArgs {
   float *part;                               // their results (attend_work_bytes)
   int32_t sinks;                             // first tokens that a window keeps visible (0: none)
   TreeView tree;                             // masks of the new tokens (null: in their order)
+  // with sinks or trees:
+  int32_t chunk;                             // tiles of a part (else parts are equal shares)
+  int32_t row_tiles;                         // workgroups that share their tokens
 };
 
 // Chooses kernel and parts (false: a row tile of all requests is no launch), and the device memory for the parts.

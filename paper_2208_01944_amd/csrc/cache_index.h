@@ -61,4 +61,20 @@ constexpr bool tile_stays_inside(int dim) {
 static_assert(tile_stays_inside(64) && tile_stays_inside(96) && tile_stays_inside(128) && tile_stays_inside(256),
               "a piece of a tile outside its block");
 
+// The tiles of 64 tokens of rows that see [lo, hi) and, before lo, the first `sinks` tokens:
+// `count` of them from number 0 on, the first tokens' before the others, so that what lies
+// between is never read.  Numbers past the last are asked for ahead (up to 8 more): their places
+// stay below 2^31 where hi is at most 2^31 - 1024, also where lo, a row's wish, lies far past hi.
+struct TileOrder {
+  int count, sink, gap;
+  constexpr int at(int i) const { return i < sink ? i : i + gap; }
+};
+constexpr TileOrder tile_order(int lo, int hi, int sinks) {
+  if (hi <= 0) return {0, 0, 0};
+  const int seen = sinks < hi ? sinks : hi, tiles = seen / 64 + (seen % 64 > 0), tile0 = lo >> 6;
+  const int sink = tiles < tile0 ? tiles : tile0;
+  if (hi <= lo) return {sink, sink, 0};
+  return {sink + (hi + 63) / 64 - tile0, sink, tile0 - sink};
+}
+
 }  // namespace palq

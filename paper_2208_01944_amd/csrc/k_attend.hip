@@ -133,12 +133,12 @@ enum { RANGE, SINKS, TREE };
 // least and the largest position that a row can have.
 struct Canopy {
   int old;            // first new token (below 0: the new ones up to there lie before the request)
-  int context;        // tokens before the new ones
+  int context, end;   // tokens before the new ones, and before the first that no bit stands for
   int low, high;      // least and largest first token of a row's range
 };
 __device__ __forceinline__ Canopy canopy_of(const AttendArgs &a, const Request &q, int r) {
   const Draft d = draft_of(a.b, r, a.tree.words);
-  Canopy c{max(d.old, -64 * PALQ_TREE_WORDS), max(0, min(d.old, q.len)), 0, 0};
+  Canopy c{max(d.old, -64 * PALQ_TREE_WORDS), max(0, min(d.old, q.len)), (int)max((int64_t)0, min((int64_t)d.old + d.n, (int64_t)q.len)), 0, 0};
   if (a.window > 0) {
     c.low = (int)max((int64_t)0, (int64_t)d.old - a.window + 1);
     c.high = (int)min(max((int64_t)0, (int64_t)d.old + d.n - a.window + 1), (int64_t)0x7fffffff);  // (a row without a bit may see all n)
@@ -168,27 +168,26 @@ __device__ __forceinline__ uint32_t first16(int n) { return n >= 16 ? 0xffffu : 
 // Which of the 16 tokens from tok on a row sees that has the range [lo, hi); of sinks, and of a tree's new tokens.
 __device__ __forceinline__ uint32_t seen16(const AttendArgs &a, const Request &q, int tok, int lo, int hi, const Canopy &cp, const uint64_t *mask) {
   uint32_t m = (first16(hi - tok) & ~first16(lo - tok)) | first16(min(a.sinks, hi) - tok);
-  if (mask && tok + 16 > cp.old) m |= bits16(mask, a.tree.words, tok - cp.old) & first16(q.len - tok);
+  if (mask && tok + 16 > cp.old) m |= bits16(mask, a.tree.words, tok - cp.old) & first16(cp.end - tok);
   return m;
 }
 
-// The tiles of 64 tokens of rows that see [lo, hi), by number; SINKS, TREE: the first tokens'
-// tiles come before the others, so a tile's number is not its place.
+// The tiles of 64 tokens that a block of rows takes, by number: RANGE: their places; else tile_order's.
 template <int SEES>
 struct Tiles {
-  int first, count, sink = 0, gap = 0;
+  int first, count;
+  TileOrder order{0, 0, 0};
   __device__ __forceinline__ Tiles(const AttendArgs &a, int lo, int hi) {
-    const int tile0 = lo >> 6, n = hi > lo ? ((hi + 63) >> 6) - tile0 : 0;
-    first = tile0;
-    count = n;
-    if constexpr (SEES != RANGE) {
-      sink = min((int)(((int64_t)min(a.sinks, hi) + 63) >> 6), tile0);
-      gap = tile0 - sink;
+    if constexpr (SEES == RANGE) {
+      first = lo >> 6;
+      count = hi > lo ? ((hi + 63) >> 6) - first : 0;
+    } else {
+      order = tile_order(lo, hi, a.sinks);
       first = 0;
-      count = sink + n;
+      count = order.count;
     }
   }
-  __device__ __forceinline__ int at(int i) const { return SEES == RANGE || i < sink ? i : i + gap; }
+  __device__ __forceinline__ int at(int i) const { return SEES == RANGE ? i : order.at(i); }
 };
 
 // The power of two that brings a row's largest magnitude (its bits) to [2^14, 2^15),
@@ -224,23 +223,41 @@ __device__ __forceinline__ h8 scaled(v4i raw, float f) {
   return o;
 }
 
+__device__ __forceinline__ float other_half_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// (of the lane 16 on, or before, in the same half)
+__device__ __forceinline__ float other_row_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // ------------------------------------------------------------ few rows
 // NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
 // fourth tile of 64 tokens; the waves join in LDS, splits in attend_join_kernel.
 // Operands go from memory straight into registers, one tile ahead.  32 requests of 2047
 // to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 117 us, 5.2 TB/s (a
 // plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 21 us.
-template <class T, int D, int NQ, int SEES>
-__global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
+template <class T, int D, int NQ, int SEES, int W>
+__global__ __launch_bounds__(64 * W, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
   constexpr int CH = D % 64 == 0 ? 16 : 8;  // consecutive channels of a key that a lane loads at once
-  __shared__ float sm[4][NQ * 16], sl[4][NQ * 16];
-  __shared__ int su[4];
-  __shared__ __attribute__((aligned(16))) float so[4][16 * OLD];
+  __shared__ float sm[W][NQ * 16], sl[W][NQ * 16];
+  __shared__ int su[W];
+  __shared__ __attribute__((aligned(16))) float so[W][16 * OLD];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4;
-  const int h = blockIdx.y, r = blockIdx.z, split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
   const CacheView &cv = a.c;
   const int heads = cv.heads;
+  int h = blockIdx.y, r = blockIdx.z, split = blockIdx.x % a.splits, rt = blockIdx.x / a.splits;
+  if constexpr (SEES != RANGE) {  // row tiles of the same tokens 8 apart: on one XCD, whose L2 then reads them once
+    const int each = 8 * a.row_tiles, at = blockIdx.x / each * 8 + blockIdx.x % 8;
+    h = at % heads;
+    r = at / heads % a.b.requests;
+    split = at / heads / a.b.requests;
+    rt = blockIdx.x % each / 8;
+    if (split >= a.splits) return;
+  }
   const Request q = request_of(a.b, r);
   const int rows = q.n * a.group, first = rt * NQ * 16;
   if (first >= rows) return;
@@ -252,14 +269,25 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
   if constexpr (SEES == TREE) {
     cp = canopy_of(a, q, r);
     rf = {cp.low, cp.context};
-    rl = {cp.high, q.len};
+    rl = {cp.high, cp.end};
   }
   const int lo = rf.lo, hi = rl.hi;
   const Tiles<SEES> tiles(a, lo, hi);
   const int tile0 = tiles.first, ntiles = tiles.count;
-  const int per = (ntiles + a.splits - 1) / a.splits;
+  const int per = SEES == RANGE ? (ntiles + a.splits - 1) / a.splits : a.chunk;
+  if (SEES != RANGE && split > 0 && split * per >= ntiles) return;  // (the join knows)
   const int tb = tile0 + min(ntiles, split * per), te = tile0 + min(ntiles, (split + 1) * per);
 
+  const int32_t *table = a.b.table + (int64_t)r * a.b.max_pages;
+  const int kc = (col >> 2) * 16, vc = c * 16;  // first tokens of the chunks this lane loads
+  auto entry = [&](int tok) __attribute__((always_inline)) { return table[(uint32_t)min(tok, hi - 1) >> cv.shift]; };
+  int kpage = 0, vpage = 0;
+  if constexpr (SEES != RANGE) {  // (with the rows and the masks: one way to memory less)
+    if (tb + wave < te) {
+      kpage = entry(tiles.at(tb + wave) * 64 + kc);
+      vpage = entry(tiles.at(tb + wave) * 64 + vc);
+    }
+  }
   // the rows' elements are on their way while the tokens' pages are looked up
   v4i raw[NQ][KS];
   int rlo[NQ], rhi[NQ];
@@ -269,7 +297,7 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     const int row = first + n * 16 + col;
     const bool live = row < rows;
     const int t = live ? row / a.group : 0, g = live ? row - t * a.group : 0;
-    const Reach s = SEES == TREE ? branch_of(a, q, cp, r, t) : reach_of(a, q, t);
+    const Reach s = reach_of(a, q, t);
     rlo[n] = s.lo;
     rhi[n] = live ? s.hi : 0;
     if constexpr (SEES == TREE) mask[n] = live ? a.tree.mask + (q.row0 + t) * a.tree.words : nullptr;
@@ -278,6 +306,15 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     const uint16_t *p = a.q + (q.row0 + t) * a.q_row + (int64_t)(h * a.group + g) * a.q_head + c * CH;
 #pragma unroll
     for (int s = 0; s < KS; ++s) raw[n][s] = load_any(p + s * 8 / CH * 4 * CH + s * 8 % CH);
+  }
+  if constexpr (SEES == TREE) {
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+      const int row = first + n * 16 + col, t = row < rows ? row / a.group : 0;
+      const Reach s = branch_of(a, q, cp, r, t);
+      rlo[n] = s.lo;
+      rhi[n] = row < rows ? s.hi : 0;
+    }
   }
   v4f O[NQ][DT];
   float M[NQ], L[NQ];
@@ -289,15 +326,11 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 #pragma unroll
     for (int d = 0; d < DT; ++d) O[n][d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   }
-  const int32_t *table = a.b.table + (int64_t)r * a.b.max_pages;
   const int pm = cv.page - 1;
   // The tile's operands one tile ahead: keys as soon as the scores have taken the
   // present ones, values after the second product, table entries (checked where
   // they are used: a branch on them would wait for every load in flight) one
   // tile before that.
-  const int kc = (col >> 2) * 16, vc = c * 16;  // first tokens of the chunks this lane loads
-  auto entry = [&](int tok) __attribute__((always_inline)) { return table[(uint32_t)min(tok, hi - 1) >> cv.shift]; };
-  int kpage = 0, vpage = 0;
   bool vthere = false;
   float ks = 0.0f, vs = 0.0f;
   uint32_t kx[4][D / 16];
@@ -336,14 +369,16 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     const int vt = tiles.at(tile) * 64 + vc;
     const bool ok = ((uint32_t)vpage < (uint32_t)cv.pages) & (vt < hi);
     const int8_t *vb = cv.v + (((int64_t)(ok ? vpage : 0) * heads + h) * D + col) * cv.page + (vt & pm);
-    kpage = entry(tiles.at(tile + 4) * 64 + kc);
-    vpage = entry(tiles.at(tile + 4) * 64 + vc);
+    kpage = entry(tiles.at(tile + W) * 64 + kc);
+    vpage = entry(tiles.at(tile + W) * 64 + vc);
 #pragma unroll
     for (int d = 0; d < DT; ++d) vx[d] = *(const v4i *)(vb + d * 16 * cv.page);
   };
   if (tb + wave < te) {
-    kpage = entry(tiles.at(tb + wave) * 64 + kc);
-    vpage = entry(tiles.at(tb + wave) * 64 + vc);
+    if constexpr (SEES == RANGE) {
+      kpage = entry(tiles.at(tb + wave) * 64 + kc);
+      vpage = entry(tiles.at(tb + wave) * 64 + vc);
+    }
     load_k(tb + wave);
     load_v(tb + wave);
   }
@@ -402,25 +437,23 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 #pragma unroll
         for (int n = 0; n < NQ; ++n) S[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, Q[n][s], S[n][j], 0, 0, 0);
       }
-    if constexpr (more) load_k(tile + 4);
+    if constexpr (more) load_k(tile + W);
     h8 P[NQ][2];
     // Tokens that all rows see need no masks (columns past the last row are not stored).
     // 8 requests of 17 to 131 rows, heads of 64: 18.5 us, 21.5 with masks always.  The wider
     // builds keep them: two paths took 256 registers and scratch (heads of 128, 32 rows).
-    const bool whole = D * NQ <= 128 && __all(there) && t0 >= rl.lo && t0 + 64 <= rf.hi;
+    const bool whole = (SEES != RANGE || D * NQ <= 128) && __all(there) && t0 >= rl.lo && t0 + 64 <= rf.hi;
     auto weigh = [&](int n, auto masks) __attribute__((always_inline)) {
       constexpr bool some = decltype(masks)::value;
       const float fk = f[n] * kst;
       float mx = -INFINITY;
-      uint32_t seen = 0;
-      if constexpr (some && SEES != RANGE) seen = there ? seen16(a, q, vt, rlo[n], rhi[n], cp, SEES == TREE ? mask[n] : nullptr) : 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (some) {
             const int tok = vt + 4 * j + i;
-            const bool sees = SEES == RANGE ? there & (tok >= rlo[n]) & (tok < rhi[n]) : seen >> (4 * j + i) & 1;
+            const bool sees = there & (tok >= rlo[n]) & (tok < rhi[n]);
             S[n][j][i] = sees ? __builtin_fmaf(S[n][j][i], fk, u) : -INFINITY;
           }
           mx = fmaxf(mx, S[n][j][i]);
@@ -448,7 +481,69 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
         }
       L[n] += sum == 0.0f ? 0.0f : sum * rv;
     };
-    if (whole) {
+    // Sinks and trees mask the products themselves, -inf times a factor above 0 (or 1, where a chunk's
+    // scales may be NaN and nothing of it is seen), so that one path without masks follows in every
+    // build, all rows together.  8 drafts of 25 tokens, heads of 96 in groups of 7, window 4095: 43 us with
+    // masks at every score, 38 so (blocks of 32 rows, no parts); 16 drafts of 64, heads of 128: 297, 254.
+    auto weigh_masked = [&]() __attribute__((always_inline)) {
+      float fk[NQ], un[NQ], mx[NQ];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        fk[n] = f[n] * kst;
+        un[n] = u;
+      }
+      if (!whole) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const uint32_t seen = there ? seen16(a, q, vt, rlo[n], rhi[n], cp, SEES == TREE ? mask[n] : nullptr) : 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[n][j][i] = seen >> (4 * j + i) & 1 ? S[n][j][i] : -INFINITY;
+          fk[n] = seen == 0 ? 1.0f : fk[n] == 0.0f ? 1.17549435e-38f : fk[n];
+          un[n] = seen == 0 ? 0.0f : u;
+        }
+      }
+      bool up = false;
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) m = fmaxf(m, S[n][j][i]);
+        m = m == -INFINITY ? -INFINITY : __builtin_fmaf(m, fk[n], un[n]);
+        mx[n] = other_half_max(other_row_max(m));
+        up |= mx[n] > M[n] + kSlack;
+      }
+      if (__any(up)) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          const float mn = fmaxf(M[n], mx[n]), alpha = exp2_fast(M[n] - (mn == -INFINITY ? 0.0f : mn));
+          M[n] = mn;
+          L[n] *= alpha;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) O[n][d] *= alpha;
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const float o = un[n] - (M[n] == -INFINITY ? 0.0f : M[n]);
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = exp2_fast(__builtin_fmaf(S[n][j][i], fk[n], o));
+            sum += p;
+            P[n][j >> 1][(j & 1) * 4 + i] = (_Float16)p;
+          }
+        L[n] += sum == 0.0f ? 0.0f : sum * rv;
+      }
+    };
+    if constexpr (SEES != RANGE) {
+      weigh_masked();
+    } else if (whole) {
 #pragma unroll
       for (int n = 0; n < NQ; ++n) weigh(n, std::false_type());
     } else {
@@ -463,11 +558,11 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 #pragma unroll
         for (int n = 0; n < NQ; ++n) O[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(A, P[n][s], O[n][d], 0, 0, 0);
       }
-    if constexpr (more) load_v(tile + 4);
+    if constexpr (more) load_v(tile + W);
   };
   // (the last step apart: under a condition, loads would be waited for as if there were none)
   int tile = tb + wave;
-  for (; tile + 4 < te; tile += 4) step(tile, std::false_type());
+  for (; tile + W < te; tile += W) step(tile, std::false_type());
   if (tile < te) step(tile, std::true_type());
 
   // the waves' results under one maximum and in one unit
@@ -483,28 +578,32 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
     }
   }
   __syncthreads();
-  const int ut = max(max(su[0], su[1]), max(su[2], su[3]));
+  int ut = max(max(su[0], su[1]), max(su[2], su[3]));
+#pragma unroll
+  for (int w = 4; w < W; ++w) ut = max(ut, su[w]);
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int rc = n * 16 + col;
-    const float mt = fmaxf(fmaxf(sm[0][rc], sm[1][rc]), fmaxf(sm[2][rc], sm[3][rc]));
+    float mt = fmaxf(fmaxf(sm[0][rc], sm[1][rc]), fmaxf(sm[2][rc], sm[3][rc]));
+#pragma unroll
+    for (int w = 4; w < W; ++w) mt = fmaxf(mt, sm[w][rc]);
     const float wgt = __builtin_ldexpf(exp2_fast(M[n] - (mt == -INFINITY ? 0.0f : mt)), unit.u - ut);
 #pragma unroll
     for (int d = 0; d < DT; ++d) *(v4f *)&so[wave][col * OLD + d * 16 + c * 4] = O[n][d] * wgt;
     __syncthreads();
-    for (int p = threadIdx.x; p < 16 * (D / 4); p += 256) {
+    for (int p = threadIdx.x; p < 16 * (D / 4); p += 64 * W) {
       const int qr = p / (D / 4), d = p % (D / 4) * 4, row = first + n * 16 + qr;
       if (row >= rows) continue;
       const int t = row / a.group, hq = h * a.group + row - t * a.group;
       v4f o = *(v4f *)&so[0][qr * OLD + d];
 #pragma unroll
-      for (int w = 1; w < 4; ++w) o += *(v4f *)&so[w][qr * OLD + d];
+      for (int w = 1; w < W; ++w) o += *(v4f *)&so[w][qr * OLD + d];
       const int rq = n * 16 + qr;
       float m = -INFINITY, l = 0.0f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) m = fmaxf(m, sm[w][rq]);
+      for (int w = 0; w < W; ++w) m = fmaxf(m, sm[w][rq]);
 #pragma unroll
-      for (int w = 0; w < 4; ++w) l += sl[w][rq] * exp2_fast(sm[w][rq] - (m == -INFINITY ? 0.0f : m));
+      for (int w = 0; w < W; ++w) l += sl[w][rq] * exp2_fast(sm[w][rq] - (m == -INFINITY ? 0.0f : m));
       if (a.splits == 1) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         const float v[4] = {__builtin_ldexpf(o[0] * inv, ut), __builtin_ldexpf(o[1] * inv, ut), __builtin_ldexpf(o[2] * inv, ut),
@@ -538,10 +637,6 @@ __global__ __launch_bounds__(256, D < 256 ? 2 : 1) void attend_rows_kernel(Atten
 // threads that bring a tile are arranged so that 8 neighbours write 8 neighbouring
 // lanes' pieces (row 8 g + 4 c + i of a subtile of keys is token 16 c + 4 g + i).
 //
-__device__ __forceinline__ float other_half_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
 
 template <int D>
 struct TileLds {
@@ -591,12 +686,13 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   if constexpr (SEES == TREE) {
     cp = canopy_of(a, q, r);
     rf = {cp.low, cp.context};
-    rl = {cp.high, q.len};
+    rl = {cp.high, cp.end};
   }
   const int hi = rl.hi;
   const Tiles<SEES> tiles(a, rf.lo, hi);
   const int tile0 = tiles.first, ntiles = tiles.count;
-  const int per = (ntiles + a.splits - 1) / a.splits;
+  const int per = SEES == RANGE ? (ntiles + a.splits - 1) / a.splits : a.chunk;
+  if (SEES != RANGE && split > 0 && split * per >= ntiles) return;  // (the join knows)
   const int tb = tile0 + min(ntiles, split * per), te = tile0 + min(ntiles, (split + 1) * per);
 
   // this wave's rows
@@ -948,7 +1044,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
 
 // One (token, head) row a group of D / 4 threads: the splits under one maximum and
 // in one unit.
-template <class T, int D>
+template <class T, int D, int SEES>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   constexpr int W = D / 4;
   const int r = blockIdx.y;
@@ -958,15 +1054,29 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   if (sub >= 256 / W || i >= (int64_t)q.n * hs) return;
   const int64_t t = i / hs, hq = i - t * hs, at = (q.row0 + t) * hs + hq, step = a.b.tokens * hs;
   const float *ml = a.part + a.splits * step * D;
+  int splits = a.splits;
+  if constexpr (SEES != RANGE) {  // the parts that the row's block has
+    const int row = (int)t * a.group + (int)hq % a.group, first = row / a.block * a.block, last = min(q.n * a.group, first + a.block) - 1;
+    int lo, hi;
+    if constexpr (SEES == TREE) {
+      const Canopy cp = canopy_of(a, q, r);
+      lo = cp.low;
+      hi = cp.end;
+    } else {
+      lo = reach_of(a, q, first / a.group).lo;
+      hi = reach_of(a, q, last / a.group).hi;
+    }
+    splits = max(1, min(splits, (Tiles<SEES>(a, lo, hi).count + a.chunk - 1) / a.chunk));
+  }
   // eight splits at a time, all their loads in flight
   float m = -INFINITY, l = 0.0f, u = kNoUnit;
   v4f o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+  for (int s0 = 0; s0 < splits; s0 += 8) {
     v4f x[8];
     v4f y[8];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      const int64_t from = min(s0 + s, a.splits - 1) * step + at;
+      const int64_t from = min(s0 + s, splits - 1) * step + at;
       x[s] = *(const v4f *)(ml + from * 4);
       y[s] = *(const v4f *)(a.part + from * D + d);
     }
@@ -983,7 +1093,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
     u = un;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      const float w = s0 + s < a.splits ? exp2_fast(x[s][0] - ms) : 0.0f;
+      const float w = s0 + s < splits ? exp2_fast(x[s][0] - ms) : 0.0f;
       l += x[s][1] * w;
       o += y[s] * __builtin_ldexpf(w, (int)(x[s][2] - u));
     }
@@ -996,14 +1106,24 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
   store4<T>(dst, v);
 }
 
+// Waves of attend_rows_kernel's workgroups: eight with sinks or trees, whose rows then need fewer parts that
+// are joined through memory (one token behind 700: 7.2 us, 8.0 with four; 32 of a window of 4096: 55.4, 56.6; 8 drafts of
+// 25: 33.5, 37.9); heads of 256 have registers for four.
+constexpr int rows_waves(int dim, int sees) { return sees != RANGE && dim < 256 ? 8 : 4; }
+
 // Rows of a workgroup: 16 or 32 on attend_rows_kernel, 128 on attend_tile_kernel.
 // While the small blocks are at most 3 for each CU, their many waves over the
 // tokens end sooner than the tile kernel's long chain of steps, although each
 // block converts its codes itself: 4 requests, 8 heads, group 4, 2048 tokens, 64 /
-// 128 / 256 new ones: 29 / 39 / 72 us against 35 / 40 / 58.
+// 128 / 256 new ones: 29 / 39 / 72 us against 35 / 40 / 58.  Drafts whose rows fill
+// blocks of 128 go there from one small block for each CU on if they are behind 8192 tokens
+// or more (4 / 8 / 12 drafts of 64 behind 8000 to 16000: 99 / 191 / 279 us, 114 / 207 / 296 in small
+// blocks; behind 1000 to 2000 64 / 67 / 67, 26 / 46 / 67).
 int block_rows(const AttendArgs &a, int cus) {
   const int64_t rows = (int64_t)a.b.max_new * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
-  return (rows + small - 1) / small * a.c.heads * a.b.requests <= 3 * cus ? (int)small : 128;
+  const int64_t blocks = (rows + small - 1) / small * a.c.heads * a.b.requests;
+  if (a.tree.mask && a.window == 0 && a.b.max_len >= 8192 && (rows + 127) / 128 * 128 * 8 <= rows * 9 && blocks >= cus) return 128;
+  return blocks <= 3 * cus ? (int)small : 128;
 }
 
 template <class T, int D, int SEES>
@@ -1019,13 +1139,15 @@ hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
       else attend_tile_kernel<T, D, false, SEES><<<flat, 256, 0, s>>>(a, (int)t0, (int)n);
     }
   } else {
-    const dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
-    if (a.block == 16) attend_rows_kernel<T, D, 1, SEES><<<g, 256, 0, s>>>(a);
-    else if constexpr (D < 256) attend_rows_kernel<T, D, 2, SEES><<<g, 256, 0, s>>>(a);
+    dim3 g((unsigned)(rt * a.splits), (unsigned)a.c.heads, (unsigned)a.b.requests);
+    if (SEES != RANGE) g = dim3((unsigned)((a.splits * a.c.heads * a.b.requests + 7) / 8 * 8 * a.row_tiles));
+    constexpr int W = rows_waves(D, SEES);
+    if (a.block == 16) attend_rows_kernel<T, D, 1, SEES, W><<<g, 64 * W, 0, s>>>(a);
+    else if constexpr (D < 256) attend_rows_kernel<T, D, 2, SEES, W><<<g, 64 * W, 0, s>>>(a);
   }
   if (a.splits > 1) {
     const int64_t per = 256 / (D / 4), n = (int64_t)a.b.max_new * a.c.heads * a.group;
-    attend_join_kernel<T, D><<<dim3((unsigned)((n + per - 1) / per), (unsigned)a.b.requests), 256, 0, s>>>(a);
+    attend_join_kernel<T, D, SEES><<<dim3((unsigned)((n + per - 1) / per), (unsigned)a.b.requests), 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -1054,11 +1176,20 @@ bool attend_plan(AttendArgs &a, int cus) {
   // rows: its waves hold twice the accumulators; 4 requests, 5 tokens, window 8191: 24 us
   // in 8 parts, 26 in 16).  A part has two tiles or more for every wave, and what is
   // done in four is not cut at all: joining costs as much.
-  // (of sinks and trees the tokens that a window leaves)
-  const bool some = (a.sinks || a.tree.mask) && a.window > 0;
-  const int64_t len = some ? std::min<int64_t>(a.b.max_len, (int64_t)a.window + a.b.max_new + a.sinks) : a.b.max_len;
-  const int64_t most = len <= 1024 ? 1 : (len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
+  const int64_t most = a.b.max_len <= 1024 ? 1 : (a.b.max_len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), want / base));
+  if (a.sinks || a.tree.mask) {
+    const int64_t len = a.window > 0 ? std::min<int64_t>(a.b.max_len, (int64_t)a.window + (a.tree.mask ? 64 * a.tree.words : a.b.max_new) + a.sinks + 128) : a.b.max_len;
+    // Parts of `chunk` tiles: a request has as many as it has tokens for, so that long ones do not go on alone (16 drafts
+    // of 64 behind 1000 to 16384 tokens: 237 us in up to 6 parts, 267 in 4, 311 in 2), a part two tiles or more for each wave.
+    // Small blocks stand one on a CU, and joining costs what a second would gain (32 of a window of 4096: 55 us in one
+    // part, 63 in two).
+    const int64_t tiles = (len + 63) / 64, least = a.block == 128 ? 32 : 2 * rows_waves(a.c.dim, SINKS);
+    const int64_t parts = (a.block == 128 ? 6 : 1) * cus / base;
+    a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(parts, 64), tiles / least));
+    a.row_tiles = (int32_t)std::min<int64_t>(rt, 0x7fffffff);
+    a.chunk = (int32_t)std::max<int64_t>(1, (tiles + a.splits - 1) / a.splits);
+  }
   return (int64_t)a.splits * a.c.heads * a.b.requests <= kMaxGroups;
 }
 

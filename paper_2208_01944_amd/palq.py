@@ -391,37 +391,52 @@ class Context:
     def norm_rotate(self, batch: Batch, q, q_out, k=None, k_out=None, q_weight=None, k_weight=None, eps=None, rotation=None, tree=None):
         """palq_norm_rotate: each head of q and k [tokens, heads, head_dim] normed (eps None: not) and rotated by position
         into q_out and k_out, which may be q and k.  tree: int64 masks [tokens, words]."""
-        tokens, _, dim = q.shape
-        kind, place = _TYPES.get(q.dtype), []
-        for x, y in ((q, q_out), (k, k_out)):
-            if (x is None) != (y is None):
-                raise PalqError(ERR_ARG, "k and k_out go together")
-            if x is None:
-                place.append((None, 0, 0, 0, None, 0, 0))
-                continue
-            xr, xh, x1 = x.stride()
-            yr, yh, y1 = y.stride()
-            if x.dtype != q.dtype or y.dtype != q.dtype or kind is None:
-                raise PalqError(ERR_ARG, "the tensors differ in type, or have no element type of the library")
-            if y.shape != x.shape or x.shape[0] != tokens or x.shape[2] != dim or x1 != 1 or y1 != 1:
-                raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim], results of their shapes, a head's channels consecutive")
-            place.append((x.data_ptr(), xr, xh, x.shape[1], y.data_ptr(), yr, yh))
-        for w in (q_weight, k_weight):
-            if w is not None:
-                _need(w, torch.float32, dim, "a weight")
-        if eps == 0:
+        tokens, qn, dim = shape = q.shape
+        dtype, d = q.dtype, self.device
+        qr, qh, q1 = q.stride()
+        qor, qoh, qo1 = q_out.stride()
+        kind = _TYPES.get(dtype)
+        if kind is None or q_out.dtype != dtype:
+            raise PalqError(ERR_ARG, "the tensors differ in type, or have no element type of the library")
+        if q_out.shape != shape or q1 != 1 or qo1 != 1:
+            raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim], results of their shapes, a head's channels consecutive")
+        on = d < 0 or (q.get_device() == d and q_out.get_device() == d and batch.device == d)
+        kp = ko = qw = kw = None
+        kr = kh = kn = kor = koh = 0
+        if k is not None and k_out is not None:
+            kt, kn, kd = shape = k.shape
+            kr, kh, k1 = k.stride()
+            kor, koh, ko1 = k_out.stride()
+            if k.dtype != dtype or k_out.dtype != dtype or kt != tokens or kd != dim or k_out.shape != shape or k1 != 1 or ko1 != 1:
+                raise PalqError(ERR_ARG, "k and k_out must be as q, [tokens, heads, head_dim]")
+            on = on and (d < 0 or (k.get_device() == d and k_out.get_device() == d))
+            kp, ko = k.data_ptr(), k_out.data_ptr()
+        elif k is not None or k_out is not None:
+            raise PalqError(ERR_ARG, "k and k_out go together")
+        if q_weight is not None:
+            _need(q_weight, torch.float32, dim, "a weight")
+            on = on and (d < 0 or q_weight.get_device() == d)
+            qw = q_weight.data_ptr()
+        if k_weight is not None:
+            _need(k_weight, torch.float32, dim, "a weight")
+            on = on and (d < 0 or k_weight.get_device() == d)
+            kw = k_weight.data_ptr()
+        if not on:
+            raise PalqError(ERR_ARG, f"tensors or batch are not on the context's device, cuda:{d}")
+        if eps is None:
+            eps = 0.0
+        elif not eps > 0:
             raise PalqError(ERR_ARG, "eps must be above 0 (None: no norm)")
-        if rotation is not None and rotation.ctx is not self:
-            raise PalqError(ERR_ARG, "rotation of another context")
-        d = self.device
-        if d >= 0:
-            _on(self, batch.lens, *(t for t in (q, q_out, k, k_out, q_weight, k_weight) if t is not None))
-        tree = _tree(self, tree, tokens)
+        if rotation is not None:
+            if rotation.ctx is not self:
+                raise PalqError(ERR_ARG, "rotation of another context")
+            rotation = rotation.h
+        if tree is not None:
+            tree = _tree(self, tree, tokens)
         if batch.tokens != tokens:
             batch.tokens = batch.desc.tokens = tokens
-        (qp, qr, qh, qn, qo, qor, qoh), (kp, kr, kh, kn, ko, kor, koh) = place
-        st = _norm_rotate(self.h, rotation.h if rotation is not None else None, batch.ref, tree, qp, qr, qh, qn, qo, qor, qoh, _ptr(q_weight),
-                          kp, kr, kh, kn, ko, kor, koh, _ptr(k_weight), dim, kind, 0.0 if eps is None else eps)
+        st = _norm_rotate(self.h, rotation, batch.ref, tree, q.data_ptr(), qr, qh, qn, q_out.data_ptr(), qor, qoh, qw, kp, kr, kh, kn, ko, kor,
+                          koh, kw, dim, kind, eps)
         if st:
             self._check(st)
 
@@ -432,27 +447,36 @@ class Context:
         kind, ld = _rows2(logits)
         if vocab > _INT_MAX:
             raise PalqError(ERR_UNSUPPORTED, "a row of 2^31 elements or more")
+        d = self.device
+        on = d < 0 or logits.get_device() == d
         given = n = 0
+        ip = op = ep = tp = lp = None
         if ids is not None:
-            given = 1 if ids.dim() == 1 else ids.shape[1]
-            _need(ids, torch.int32, rows * given, "ids")
-            if out is None or ids.shape[0] != rows or out.shape != ids.shape:
+            shape = ids.shape
+            given = shape[1] if len(shape) == 2 else 1
+            if out is None or shape[0] != rows or out.shape != shape:
                 raise PalqError(ERR_ARG, "ids must have a row for each of the logits', and out their shape")
+            _need(ids, torch.int32, rows * given, "ids")
             _need(out, torch.float32, rows * given, "out")
-        if (top_ids is None) != (top is None):
-            raise PalqError(ERR_ARG, "top_ids and top go together")
-        if top is not None:
-            n = top.shape[1]
-            _need(top_ids, torch.int32, rows * n, "top_ids")
-            _need(top, torch.float32, rows * n, "top")
-            if top.shape[0] != rows or top_ids.shape != top.shape:
-                raise PalqError(ERR_ARG, "top_ids and top must be [rows, n]")
+            on = on and (d < 0 or (ids.get_device() == d and out.get_device() == d))
+            ip, op = ids.data_ptr(), out.data_ptr()
         if entropy is not None:
             _need(entropy, torch.float32, rows, "entropy")
-        if self.device >= 0:
-            _on(self, logits, *(t for t in (ids, out, entropy, top_ids, top) if t is not None))
-        st = _log_probs(self.h, logits.data_ptr(), kind, rows, vocab, ld, scale, _ptr(ids), given, _ptr(out if given else None),
-                        _ptr(entropy), n, _ptr(top_ids), _ptr(top))
+            on = on and (d < 0 or entropy.get_device() == d)
+            ep = entropy.data_ptr()
+        if top is not None and top_ids is not None:
+            m, n = shape = top.shape
+            if m != rows or top_ids.shape != shape:
+                raise PalqError(ERR_ARG, "top_ids and top must be [rows, n]")
+            _need(top_ids, torch.int32, rows * n, "top_ids")
+            _need(top, torch.float32, rows * n, "top")
+            on = on and (d < 0 or (top_ids.get_device() == d and top.get_device() == d))
+            tp, lp = top_ids.data_ptr(), top.data_ptr()
+        elif top is not None or top_ids is not None:
+            raise PalqError(ERR_ARG, "top_ids and top go together")
+        if not on:
+            raise PalqError(ERR_ARG, f"tensors are not on the context's device, cuda:{d}")
+        st = _log_probs(self.h, logits.data_ptr(), kind, rows, vocab, ld, scale, ip, given, op, ep, n, tp, lp)
         if st:
             self._check(st)
 
@@ -598,12 +622,12 @@ def _together(*tensors):
 
 def _tree(ctx, t, tokens):
     """Masks of a tree of drafted tokens, int64 [tokens, words], as the library takes them."""
-    if t is None:
-        return None
-    if t.dtype != torch.int64 or t.dim() != 2 or t.shape[0] != tokens or not t.is_contiguous():
+    shape = t.shape
+    if t.dtype != torch.int64 or len(shape) != 2 or shape[0] != tokens or not t.is_contiguous():
         raise PalqError(ERR_ARG, "tree must be contiguous int64 [tokens, words]")
-    _on(ctx, t)
-    return ctypes.byref(TreeDesc(t.data_ptr(), t.shape[1]))
+    if ctx.device >= 0 and t.get_device() != ctx.device:
+        _on(ctx, t)
+    return ctypes.byref(TreeDesc(t.data_ptr(), shape[1]))
 
 
 def _rows2(t):
