@@ -589,7 +589,7 @@ palq_status palq_log_probs(palq_ctx *ctx, const void *logits, int32_t type, int6
       if (overlaps(t[i].p, t[i].bytes, t[j].p, t[j].bytes)) return fail(ctx, PALQ_ERR_ARG, "log probabilities: an output overlaps another tensor");
   if (ctx->device < 0 || rows == 0) return PALQ_OK;
   hipSetDevice(ctx->device);
-  ScoreArgs a{logits, rows, ld, vocab, scale, ids, given, out, entropy, top, top_ids, top_out, 1, 1, nullptr};
+  ScoreArgs a{logits, rows, ld, vocab, scale, ids, given, out, entropy, top, top_ids, top_out, 0, 0, 1, nullptr};
   score_plan(a, ctx->cus);
   if (const size_t need = score_work_bytes(a)) {
     a.part = (float *)workspace(ctx, need);

@@ -17,7 +17,8 @@ struct ScoreArgs {
   int32_t top;
   int32_t *top_ids;                // [rows][top]
   float *top_out;
-  int32_t splits, each;            // parts of a row, of `each` steps
+  int32_t step;                    // logits of a wave's step
+  int32_t splits, each;            // parts of a row, of four waves with `each` steps; 0: a row is one wave's
   float *part;                     // their results (score_work_bytes)
 };
 
