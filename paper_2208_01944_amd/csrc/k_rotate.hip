@@ -129,38 +129,46 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first
   constexpr int HEADS = 64 / L;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & (L - 1), sub = (threadIdx.x & 63) / L;
   const int r = blockIdx.y;
+  const bool there = 16 * lane < a.dim;
+  const int mine = there ? lane : 0;
+  uint64_t phase[8];  // (before the request is known: one way to memory less)
+#pragma unroll
+  for (int i = 0; i < 8; ++i) phase[i] = 8 * mine + i < a.pairs ? a.phase[8 * mine + i] : 0;
   const Request q = request_of(a.b, r);
   const uint32_t share = blockIdx.x * 4 + wave, rank = share / (uint32_t)parts;  // (below 2^26)
   if (first_row + rank >= q.n) return;
   const int t = (int)(first_row + rank), part = (int)(share - rank * parts);
   const int64_t row = q.row0 + t;
+  const int q_blocks = (a.heads[0] + HEADS - 1) / HEADS, blocks = q_blocks + (a.heads[1] + HEADS - 1) / HEADS;
+  const int from = part * each, to = min(from + each, blocks);
+  typedef typename T::raw Raw;
+  // a block's heads, asked for before the angles, or the block before it, are ready
+  Lane<T, FORM> next;
+  auto load = [&](int b) __attribute__((always_inline)) {
+    const int which = b >= q_blocks, h = (b - (which ? q_blocks : 0)) * HEADS + sub, hh = there && h < a.heads[which] ? h : 0;
+    next.load((const Raw *)a.x[which] + row * a.x_row[which] + hh * a.x_head[which], mine, a.pairs);
+  };
+  if (from < to) load(from);
   int64_t pos = q.pos + (int64_t)t;
   if (a.tree.mask) {
     const Draft d = draft_of(a.b, r, a.tree.words);
     pos = (int64_t)d.old + depth_of(a.tree.mask + row * a.tree.words, a.tree.words, d.n, (int)min((int64_t)d.first + t, (int64_t)1 << 30));
   }
-  const bool there = 16 * lane < a.dim;
-  const int mine = there ? lane : 0;
   float c[8], s[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int p = 8 * mine + i;
-    const Turn u = p < a.pairs ? turn_of((uint64_t)pos * a.phase[p]) : Turn{1.0f, 0.0f};
+    const Turn u = turn_of((uint64_t)pos * phase[i]);  // (0 turns past the pairs)
     c[i] = u.c;
     s[i] = u.s;
   }
-  const int q_blocks = (a.heads[0] + HEADS - 1) / HEADS, blocks = q_blocks + (a.heads[1] + HEADS - 1) / HEADS;
-  const int from = part * each, to = min(from + each, blocks);
   Lane<F32, FORM> w;
   int have = -1;
-  typedef typename T::raw Raw;
   const float mean = 1.0f / (float)a.dim;
   for (int b = from; b < to; ++b) {
     const int which = b >= q_blocks, h = (b - (which ? q_blocks : 0)) * HEADS + sub;
     const bool live = there && h < a.heads[which];
-    const int hh = live ? h : 0;
-    Lane<T, FORM> x;
-    x.load((const Raw *)a.x[which] + row * a.x_row[which] + hh * a.x_head[which], mine, a.pairs);
+    Lane<T, FORM> x = next;
+    if (b + 1 < to) load(b + 1);
     if (a.eps != 0.0f) {
       if (have != which && a.w[which]) w.load(a.w[which], mine, a.pairs);
       have = which;
