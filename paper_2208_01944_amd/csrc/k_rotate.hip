@@ -54,10 +54,10 @@ __device__ __forceinline__ float lanes_sum(float x) {
   return x;
 }
 
-// Channels of a lane's pair i of 8, p the pair's index within the head.  HALVES: channel p
-// with p + pairs, eight of each in a row; NEIGHBOURS: 2 p with 2 p + 1, sixteen in a row;
-// MIXED: halves that eight does not divide, an element at a time.  Past the rotating pairs
-// all take 2 p and 2 p + 1.
+// Channels of a lane.  HALVES: of 8 pairs, channel p with p + pairs, eight of each in a row (past the rotating
+// pairs sixteen in a row).  NEIGHBOURS: 8 pairs of 2 p with 2 p + 1, sixteen in a row.  MIXED: halves that eight
+// does not divide: sixteen in a row, each with its partner's value from LDS and its own angle (22.5 k tokens, 40 heads
+// of 128: 138 us for 60 pairs, 95 for 64 in HALVES).
 enum { HALVES, NEIGHBOURS, MIXED };
 
 template <class T>
@@ -80,45 +80,26 @@ __device__ __forceinline__ void store8<BF16>(uint16_t *p, const float *v) {
   store_any(p, o);
 }
 
-// 16 channels of a lane as 8 pairs: first elements, then second ones.
+// 16 channels of a lane in two runs of eight.
 template <class T, int FORM>
 struct Lane {
   float v[16];
-  // first channels of the two runs of eight
   static __device__ __forceinline__ void runs(int lane, int pairs, int &a, int &b) {
     const bool rot = FORM == HALVES && 8 * lane < pairs;
     a = rot ? 8 * lane : 16 * lane;
     b = rot ? a + pairs : a + 8;
   }
-  static __device__ __forceinline__ int first(int p, int pairs) { return FORM == MIXED && p < pairs ? p : 2 * p; }
-  static __device__ __forceinline__ int second(int p, int pairs) { return FORM == MIXED && p < pairs ? p + pairs : 2 * p + 1; }
   __device__ __forceinline__ void load(const typename T::raw *x, int lane, int pairs) {
-    if constexpr (FORM == MIXED) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[i] = T::get(x[first(8 * lane + i, pairs)]);
-        v[8 + i] = T::get(x[second(8 * lane + i, pairs)]);
-      }
-    } else {
-      int a, b;
-      runs(lane, pairs, a, b);
-      load8<T>(x + a, v);
-      load8<T>(x + b, v + 8);
-    }
+    int a, b;
+    runs(lane, pairs, a, b);
+    load8<T>(x + a, v);
+    load8<T>(x + b, v + 8);
   }
   __device__ __forceinline__ void store(typename T::raw *y, int lane, int pairs) const {
-    if constexpr (FORM == MIXED) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        y[first(8 * lane + i, pairs)] = T::put(v[i]);
-        y[second(8 * lane + i, pairs)] = T::put(v[8 + i]);
-      }
-    } else {
-      int a, b;
-      runs(lane, pairs, a, b);
-      store8<T>(y + a, v);
-      store8<T>(y + b, v + 8);
-    }
+    int a, b;
+    runs(lane, pairs, a, b);
+    store8<T>(y + a, v);
+    store8<T>(y + b, v + 8);
   }
 };
 
@@ -131,9 +112,14 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first
   const int r = blockIdx.y;
   const bool there = 16 * lane < a.dim;
   const int mine = there ? lane : 0;
-  uint64_t phase[8];  // (before the request is known: one way to memory less)
+  constexpr int ANGLES = FORM == MIXED ? 16 : 8;
+  __shared__ float turned[FORM == MIXED ? 4 : 1][FORM == MIXED ? 64 * 17 : 1];
+  uint64_t phase[ANGLES];  // (before the request is known: one way to memory less)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) phase[i] = 8 * mine + i < a.pairs ? a.phase[8 * mine + i] : 0;
+  for (int i = 0; i < ANGLES; ++i) {
+    const int e = ANGLES * mine + i, p = FORM == MIXED && e >= a.pairs ? e - a.pairs : e;
+    phase[i] = p < a.pairs ? a.phase[p] : 0;
+  }
   const Request q = request_of(a.b, r);
   const uint32_t share = blockIdx.x * 4 + wave, rank = share / (uint32_t)parts;  // (below 2^26)
   if (first_row + rank >= q.n) return;
@@ -154,12 +140,12 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first
     const Draft d = draft_of(a.b, r, a.tree.words);
     pos = (int64_t)d.old + depth_of(a.tree.mask + row * a.tree.words, a.tree.words, d.n, (int)min((int64_t)d.first + t, (int64_t)1 << 30));
   }
-  float c[8], s[8];
+  float c[ANGLES], s[ANGLES];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const Turn u = turn_of((uint64_t)pos * phase[i]);  // (0 turns past the pairs)
+  for (int i = 0; i < ANGLES; ++i) {
+    const Turn u = turn_of((uint64_t)pos * phase[i]);
     c[i] = u.c;
-    s[i] = u.s;
+    s[i] = FORM == MIXED && 16 * mine + i < a.pairs ? -u.s : u.s;
   }
   Lane<F32, FORM> w;
   int have = -1;
@@ -196,13 +182,26 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first
       }
     }
     Lane<T, FORM> y = x;
+    if constexpr (FORM == MIXED) {  // (17 words for 16 channels keep banks apart)
+      float *mem = turned[wave] + sub * L * 17;
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      constexpr bool near = FORM == NEIGHBOURS;
-      const int ia = near ? 2 * i : i, ib = near ? 2 * i + 1 : 8 + i;
-      if (8 * mine + i < a.pairs) {
-        y.v[ia] = __builtin_fmaf(x.v[ia], c[i], -(x.v[ib] * s[i]));
-        y.v[ib] = __builtin_fmaf(x.v[ib], c[i], x.v[ia] * s[i]);
+      for (int i = 0; i < 16; ++i) mem[17 * lane + i] = x.v[i];
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int e = 16 * mine + i, o = e < a.pairs ? e + a.pairs : e - a.pairs;
+        if (e < 2 * a.pairs) y.v[i] = __builtin_fmaf(x.v[i], c[i], mem[o + (o >> 4)] * s[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        constexpr bool near = FORM == NEIGHBOURS;
+        const int ia = near ? 2 * i : i, ib = near ? 2 * i + 1 : 8 + i;
+        if (8 * mine + i < a.pairs) {
+          y.v[ia] = __builtin_fmaf(x.v[ia], c[i], -(x.v[ib] * s[i]));
+          y.v[ib] = __builtin_fmaf(x.v[ib], c[i], x.v[ia] * s[i]);
+        }
       }
     }
     if (live) y.store((Raw *)a.y[which] + row * a.y_row[which] + h * a.y_head[which], mine, a.pairs);
