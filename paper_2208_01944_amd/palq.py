@@ -34,6 +34,7 @@ NET_KEEP_ALL, NET_TIMING, NET_GRAPH, NET_PIXEL_LAYOUT = 1, 2, 4, 8
 LAYOUT_PIXEL, LAYOUT_GROUP = 0, 1
 F32, F16, BF16, I8 = 0, 1, 2, 3  # element types of the transformer operators
 _INT_MAX = (1 << 31) - 1
+_F32, _I32 = torch.float32, torch.int32
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
 
 
@@ -396,7 +397,7 @@ class Context:
         qr, qh, q1 = q.stride()
         qor, qoh, qo1 = q_out.stride()
         kind = _TYPES.get(dtype)
-        if kind is None or q_out.dtype != dtype:
+        if kind is None or q_out.dtype is not dtype:
             raise PalqError(ERR_ARG, "the tensors differ in type, or have no element type of the library")
         if q_out.shape != shape or q1 != 1 or qo1 != 1:
             raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim], results of their shapes, a head's channels consecutive")
@@ -407,18 +408,20 @@ class Context:
             kt, kn, kd = shape = k.shape
             kr, kh, k1 = k.stride()
             kor, koh, ko1 = k_out.stride()
-            if k.dtype != dtype or k_out.dtype != dtype or kt != tokens or kd != dim or k_out.shape != shape or k1 != 1 or ko1 != 1:
+            if k.dtype is not dtype or k_out.dtype is not dtype or kt != tokens or kd != dim or k_out.shape != shape or k1 != 1 or ko1 != 1:
                 raise PalqError(ERR_ARG, "k and k_out must be as q, [tokens, heads, head_dim]")
             on = on and (d < 0 or (k.get_device() == d and k_out.get_device() == d))
             kp, ko = k.data_ptr(), k_out.data_ptr()
         elif k is not None or k_out is not None:
             raise PalqError(ERR_ARG, "k and k_out go together")
         if q_weight is not None:
-            _need(q_weight, torch.float32, dim, "a weight")
+            if q_weight.dtype is not _F32 or q_weight.shape != (dim,) or not q_weight.is_contiguous():
+                raise PalqError(ERR_ARG, "a weight must be head_dim contiguous values of torch.float32")
             on = on and (d < 0 or q_weight.get_device() == d)
             qw = q_weight.data_ptr()
         if k_weight is not None:
-            _need(k_weight, torch.float32, dim, "a weight")
+            if k_weight.dtype is not _F32 or k_weight.shape != (dim,) or not k_weight.is_contiguous():
+                raise PalqError(ERR_ARG, "a weight must be head_dim contiguous values of torch.float32")
             on = on and (d < 0 or k_weight.get_device() == d)
             kw = k_weight.data_ptr()
         if not on:
@@ -456,20 +459,21 @@ class Context:
             given = shape[1] if len(shape) == 2 else 1
             if out is None or shape[0] != rows or out.shape != shape:
                 raise PalqError(ERR_ARG, "ids must have a row for each of the logits', and out their shape")
-            _need(ids, torch.int32, rows * given, "ids")
-            _need(out, torch.float32, rows * given, "out")
+            if ids.dtype is not _I32 or out.dtype is not _F32 or len(shape) > 2 or not (ids.is_contiguous() and out.is_contiguous()):
+                raise PalqError(ERR_ARG, "ids must be contiguous int32, out contiguous float32")
             on = on and (d < 0 or (ids.get_device() == d and out.get_device() == d))
             ip, op = ids.data_ptr(), out.data_ptr()
         if entropy is not None:
-            _need(entropy, torch.float32, rows, "entropy")
+            if entropy.dtype is not _F32 or entropy.shape != (rows,) or not entropy.is_contiguous():
+                raise PalqError(ERR_ARG, "entropy must be a contiguous float32 for each row")
             on = on and (d < 0 or entropy.get_device() == d)
             ep = entropy.data_ptr()
         if top is not None and top_ids is not None:
             m, n = shape = top.shape
             if m != rows or top_ids.shape != shape:
                 raise PalqError(ERR_ARG, "top_ids and top must be [rows, n]")
-            _need(top_ids, torch.int32, rows * n, "top_ids")
-            _need(top, torch.float32, rows * n, "top")
+            if top_ids.dtype is not _I32 or top.dtype is not _F32 or not (top_ids.is_contiguous() and top.is_contiguous()):
+                raise PalqError(ERR_ARG, "top_ids must be contiguous int32, top contiguous float32")
             on = on and (d < 0 or (top_ids.get_device() == d and top.get_device() == d))
             tp, lp = top_ids.data_ptr(), top.data_ptr()
         elif top is not None or top_ids is not None:
