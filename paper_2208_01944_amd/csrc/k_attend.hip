@@ -737,7 +737,13 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
   // one to the other would wait for them, and so for every load before them).
   // WIDE (pages of a tile or more): the entries are the same for all threads and stay in
   // scalar registers, as do the pages' addresses.
-  struct Entries { int k[WIDE ? 1 : PP], v[WIDE ? 1 : PP], b; } ent[2];
+  // With sinks or trees narrow pages' entries do, too, where heads have 64 or 256 channels: four chunks' of a
+  // tile, its values' kept from its keys', and a thread selects its pieces' pages.  That takes vector instructions and
+  // registers for scalar ones: 4 prompts, window 1024, pages of 32: 141 us against 161 for heads of 64, 665 against 737
+  // for 256, but 223 against 216 for 128 and 216 against 190 for 96.
+  constexpr bool CHUNKS = !WIDE && SEES != RANGE && (D == 64 || D == 256);
+  struct Entries { int k[WIDE ? 1 : CHUNKS ? 4 : PP], v[WIDE || CHUNKS ? 1 : PP], b; } ent[2];
+  int vpages[CHUNKS ? 4 : 1];
   v4i kx[PP], vx[PP];
   float bks, bvs, bthere;  // of chunk threadIdx.x % 4 of tile p
   const uint32_t page_bytes = (uint32_t)heads << cv.shift;  // (times D)
@@ -749,6 +755,12 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       const ScalarInts st = (ScalarInts)(uintptr_t)table;
       e.k[0] = e.b = st[__builtin_amdgcn_readfirstlane((uint32_t)min(tiles.at(p) * 64, hi - 1) >> cv.shift)];
       e.v[0] = st[__builtin_amdgcn_readfirstlane((uint32_t)min(tiles.at(max(p - 1, tb)) * 64, hi - 1) >> cv.shift)];
+      return;
+    }
+    if constexpr (CHUNKS) {
+      const ScalarInts st = (ScalarInts)(uintptr_t)table;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e.k[j] = st[__builtin_amdgcn_readfirstlane((uint32_t)min(tiles.at(p) * 64 + j * 16, hi - 1) >> cv.shift)];
       return;
     }
 #pragma unroll
@@ -773,6 +785,30 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
       bks = ((ScalarFloats)(uintptr_t)cv.ks)[at];
       bvs = ((ScalarFloats)(uintptr_t)cv.vs)[at];
       bthere = valid(e.b) ? 1.0f : 0.0f;
+      return;
+    }
+    if constexpr (CHUNKS) {
+      // the start of the page that holds 16 tokens from chunk 16 on
+      auto page_of = [&](const int *ids, const int8_t *base, int chunk) __attribute__((always_inline)) {
+        uint64_t at[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) at[j] = (uint64_t)base + (uint64_t)(uint32_t)(valid(ids[j]) ? ids[j] : 0) * page_bytes * D;
+        const uint64_t even = chunk & 2 ? at[2] : at[0], odd = chunk & 2 ? at[3] : at[1];
+        return (const int8_t *)(chunk & 1 ? odd : even);
+      };
+      const int8_t *vp = page_of(vpages, vh, piece(0).vt >> 4);  // (a thread's pieces are 256 apart: the same tokens)
+#pragma unroll
+      for (int i = 0; i < PP; ++i) {
+        const TilePiece pc = piece(i);
+        kx[i] = *(const v4i *)(page_of(e.k, kh, pc.tok >> 4) + tile_key_at(pc, ktile, pm, D));
+        vx[i] = *(const v4i *)(vp + tile_value_at(pc, vtile, pm, cv.shift));
+      }
+      const int c4 = threadIdx.x & 3, even = c4 & 2 ? e.k[2] : e.k[0], odd = c4 & 2 ? e.k[3] : e.k[1], id = c4 & 1 ? odd : even;
+      const int chunk = tiles.at(p) * 64 + c4 * 16;  // (what no row sees sets no unit)
+      const int64_t at = (int64_t)(valid(id) ? id : 0) * heads + h;
+      bks = cv.ks[at];
+      bvs = cv.vs[at];
+      bthere = valid(id) && (chunk + 16 > rf.lo || chunk < a.sinks) ? 1.0f : 0.0f;
       return;
     }
 #pragma unroll
@@ -851,6 +887,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
         *(h8 *)(vd + 1024) = codes_h8((uint32_t)vx[i][2], (uint32_t)vx[i][3], factor, less);
       }
     }
+    if constexpr (CHUNKS)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vpages[j] = ent[odd].k[j];
     entries(p + 2, ent[odd]);
     load(p + 1, ent[odd ^ 1]);
   };
@@ -938,7 +977,14 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     // s fk + lv, fk >= 0: the largest comes from the largest product.  Of lv only the fraction, so that a
     // wide tile's whole powers of two (up to 4) take nothing from the others, and the largest weight is a
     // power of two, which fp16 holds exactly: rows with few tokens gain most.
-    const float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
+    float fk[2] = {f * b0.x, f * b1.x}, lv[2] = {b0.y, b1.y};
+    if (SEES != RANGE && masked)  // (as in attend_rows_kernel: -inf times a factor above 0 needs no second mask)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bool none = (off >> (u * 16) & 0xffffu) == 0xffffu;
+        fk[u] = none ? 1.0f : fk[u] == 0.0f ? 1.17549435e-38f : fk[u];
+        lv[u] = none ? 0.0f : lv[u];
+      }
     float mx = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -973,7 +1019,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
         L += sum == 0.0f ? 0.0f : sum * (u ? b1.z : b0.z);
       }
     };
-    if (masked) weights(std::true_type());
+    if (SEES == RANGE && masked) weights(std::true_type());
     else weights(std::false_type());
   };
 
@@ -982,6 +1028,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attend_tile_kernel(Atten
     constexpr std::integral_constant<int, 1> odd;
     entries(tb, ent[0]);
     entries(tb + 1, ent[1]);
+    if constexpr (CHUNKS)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vpages[j] = ent[0].k[j];
     load(tb, ent[0]);
     bring_blocks(tb, even);
     bring(tb, even);  // (there are no values yet: those of tile tb, twice)
