@@ -218,3 +218,29 @@ def test_wild_batches_stay_inside(palq):
             palq.attention(pair.gpu, q, out, b, 0.1, window=window, sinks=sinks)
             palq.attention(pair.gpu, q, out, b, 0.1, window=window, sinks=sinks, tree=tree)
     palq.sync()
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0])
+@pytest.mark.parametrize("words", [0, 1])
+@pytest.mark.parametrize("page,dim,heads,group,lens,new", [(16, 64, 2, 2, [90, 300], [5, 20]), (64, 128, 2, 4, [90, 300], [12, 60]),
+                                                          (32, 256, 1, 2, [200], [30]), (16, 128, 16, 2, [128, 350, 131, 300, 129, 200, 140],
+                                                                                         [64, 40, 64, 60, 1, 64, 60]),
+                                                          (32, 64, 16, 2, [128, 350, 131, 300, 129, 200, 140], [128, 40, 131, 100, 1, 64, 120])])
+def test_scales_of_scores_and_blocks(palq, page, dim, heads, group, lens, new, scale, words):
+    """Negative and zero score scales, blocks of scales far apart and of 0, in every kernel."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("scales", page, dim, heads, group, scale, words)
+    g = np.random.default_rng(dim + words)
+    table, pages = paged(g, lens, page)
+    pair = Pair(P, pages, heads, page, dim)
+    pair.fill(g, table, lens, 2.0)
+    pair.ref.ks[table[0][1]], pair.ref.vs[table[-1][0]] = 0, 0
+    pair.upload()
+    starts = cumsum(new)
+    masks = random_masks(g, lens, starts, words) if words else None
+    q = dev(g.standard_normal((starts[-1], heads * group, dim)) * 0.3, "bf16")
+    out = torch.empty_like(q)
+    palq.attention(pair.gpu, q, out, pair.batch(table, lens, starts), scale, window=50, sinks=5, tree=masks_dev(masks) if words else None)
+    palq.sync()
+    check_attend(Sees(pair.ref, masks), host(out), table, lens, starts, host(q), scale, "bf16", window=50, sinks=5)

@@ -294,3 +294,29 @@ def test_log_probs_without_parts(palq):
     palq.log_probs(x, None, None)
     palq.sync()
     assert np.abs(host(ent) - want[1]).max() < 1e-5 and np.abs(host(one) - want[0][:, 0]).max() < 1e-5
+
+
+@pytest.mark.parametrize("dtype,rows,vocab,top", [("bf16", 600, 9001, 20), ("f32", 600, 4099, 64), ("f16", 70, 140001, 64), ("f32", 2, 200003, 33),
+                                                  ("bf16", 1, 262144, 64), ("bf16", 4099, 6000, 64), ("f32", 4099, 4097, 1)])
+def test_log_probs_every_kernel(palq, dtype, rows, vocab, top):
+    """A wave a row, four, and parts of rows that are joined; long and short steps."""
+    say("log_probs kernels", dtype, rows, vocab, top)
+    g = np.random.default_rng(vocab)
+    x = dev(g.standard_normal((rows, vocab)).astype(np.float32) * 3, dtype)
+    x[:, vocab - vocab // 40:] = -np.inf
+    some = np.unique(np.r_[0, rows - 1, g.integers(0, rows, 40)])
+    ids = g.integers(0, vocab, (rows, 1))
+    got = score(palq, x, ids, top, 0.8)
+    check_scores(host(x[some]), 0.8, ids[some], tuple(t[some] for t in got), top)
+
+
+@pytest.mark.parametrize("rows", [3, 700, 4100])
+def test_log_probs_values_in_masses(palq, rows):
+    """Rows of one value, of two, and rising ones, by every kernel: the first indices of equal values."""
+    x = np.zeros((rows, 5000), np.float32)
+    x[1, ::3] = 1
+    x[2] = np.arange(5000) // 7
+    d = dev(x, "bf16")
+    got = score(palq, d, np.zeros((rows, 1), np.int64), 64)
+    some = [0, 1, 2, rows - 1]
+    check_scores(host(d[some]), 1.0, np.zeros((4, 1), np.int64), tuple(t[some] for t in got), 64)
