@@ -18,17 +18,15 @@ def test_tiles_with_sinks(tmp_path, hi, sinks):
     for (long long i = 0; i < t.count + 9LL; i += (i < 20 || i > t.count - 20) ? 1 : 100003)
       std::printf("%lld %lld\\n", i, i < t.sink ? i : i + (long long)t.gap);
   }}""" for lo in los)
-    lines = evaluate(tmp_path, body)
-    at = 0
+    lines, at = evaluate(tmp_path, body), 0
     for lo in los:
         count, sink, gap = lines[at]
         at += 1
-        first = -(-min(sinks, hi) // 64) if hi > 0 else 0
+        first = -(-min(sinks, hi) // 64) if hi > 0 else 0  # tiles of the first tokens
         rest = range(lo // 64, -(-hi // 64)) if hi > lo else range(0)
+        assert count == min(first, lo // 64) + len(rest)
         if hi <= 700:
-            want = sorted(set(range(min(first, lo // 64))) | set(rest))
-            assert [lines[at + i][1] for i in range(count)] == want, (lo, hi, sinks)
-        assert count == min(first, lo // 64) + len(rest) if hi > 0 else count == 0
+            assert [lines[at + i][1] for i in range(count)] == list(range(min(first, lo // 64))) + list(rest), (lo, hi, sinks)
         while at < len(lines) and len(lines[at]) == 2:
             i, place = lines[at]
             assert 0 <= place * 64 and place * 64 + 63 < 2 ** 31, (lo, hi, sinks, i)
