@@ -650,10 +650,11 @@ palq_status palq_attention_tree(palq_ctx *ctx, const palq_cache *cache, const pa
  * all device.  A token of logit -inf has l = -inf and counts 0 in the entropy; a
  * row of nothing else has l = -inf throughout and entropy 0.  A row with NaN or
  * +inf has NaN for every l and its entropy, and -1 for its top ids.  Sums are fp32
- * under the row's largest logit; results do not depend on how a row is cut.
- * Few rows are split and joined in the context's workspace, which may grow
- * (never while a graph is captured: PALQ_ERR_NOMEM then; run the shape once
- * before). */
+ * under the row's largest logit.  Few rows are split and joined in the context's
+ * workspace, which may grow (never while a graph is captured: PALQ_ERR_NOMEM
+ * then; run the shape once before); where a row is cut moves l and the entropy by
+ * their rounding, the list not at all.  Graphs that hold calls of one context, these or
+ * attention's, share its workspace: they are replayed one after the other. */
 #define PALQ_TOP_MAX 64
 palq_status palq_log_probs(palq_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t vocab, int64_t ld, float scale,
                            const int32_t *ids, int32_t given, float *out, float *entropy, int32_t top, int32_t *top_ids, float *top_out);

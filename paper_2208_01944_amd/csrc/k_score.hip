@@ -11,13 +11,15 @@
 //
 // The k largest.  A logit and its index as one 64-bit key (the value in the order of
 // integers, then the index from above) have no ties, so any order of work gives the
-// same list.  A wave keeps the 64 largest keys sorted, one a lane.  A step's maxima are
-// compared with the k-th; only where one passes are single logits looked at, and
-// those that pass are collected in LDS until they are sorted (bitonic, 21 exchanges
-// between lanes, all in registers) and merged (7 more).  The first step takes its bound from the k-th
-// largest of the lanes' own maxima.  Of n logits in random order k ln(n / k) pass.
+// same list.  A bound on the keys runs along: at first the k-th of the lanes' own largest
+// logits of a step, then the k-th key held.  A step's maxima are compared with it; only where
+// one passes are single logits looked at, and those that pass wait in LDS until there are
+// more than k by some, and are cut to the k largest.  Of n logits in random order
+// k ln(n / k) pass.
 //
-// Bound by memory, with 10 vector operations an element beside it.
+// Large calls are bound by memory and by 11 vector instructions a logit (82 % of the time; 4096
+// rows of 131071 with 20 alternatives 210 us, 5.1 TB/s, 200 without); small ones by a wave's
+// chain of instructions (one such row 11.5 us in two launches, 333 rows of 1000 6.6).
 #include <algorithm>
 #include <float.h>
 
