@@ -516,7 +516,7 @@ void score_plan(ScoreArgs &a, int cus) {
   a.step = total >= (int64_t)4 * cus ? kLongStep : kShortStep;
   const int32_t n = steps(a.step);
   const int64_t waves = a.rows >= (int64_t)2 * cus ? 4 : std::max<int64_t>(4, std::min<int64_t>(n, (int64_t)16 * cus / a.rows));
-  a.each = (int32_t)std::max<int64_t>((n + waves - 1) / waves, (n + 511) / 512);
+  a.each = (int32_t)std::max<int64_t>((n + (waves == 4 ? 3 : waves / 2)) / waves, (n + 511) / 512);
   a.splits = (n + 4 * a.each - 1) / (4 * a.each);
 }
 
