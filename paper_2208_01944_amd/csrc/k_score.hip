@@ -510,12 +510,13 @@ void score_plan(ScoreArgs &a, int cus) {
     a.each = steps(a.step);
     return;
   }
-  // Else workgroups of four waves, in long steps where one for each wave still puts a wave on every SIMD; one workgroup
-  // a row, without a join, from two rows a CU on, else up to four waves a SIMD.
+  // Else workgroups of four waves, in long steps where one for each wave still puts a wave on every SIMD, or two for each
+  // make one workgroup; one workgroup a row, without a join, from two rows a CU on and up to 16 steps (one row of 4000,
+  // 8000 and 16000: 7.6, 7.6 and 9.6 us, in parts 10.4, 11.3 and 11.2), else up to four waves a SIMD.
   const int64_t total = a.rows * steps(kLongStep);
-  a.step = total >= (int64_t)4 * cus ? kLongStep : kShortStep;
+  a.step = total >= (int64_t)4 * cus || (steps(kLongStep) >= 3 && steps(kLongStep) <= 8) ? kLongStep : kShortStep;
   const int32_t n = steps(a.step);
-  const int64_t waves = a.rows >= (int64_t)2 * cus ? 4 : std::max<int64_t>(4, std::min<int64_t>(n, (int64_t)16 * cus / a.rows));
+  const int64_t waves = a.rows >= (int64_t)2 * cus || n <= 16 ? 4 : std::max<int64_t>(4, std::min<int64_t>(n, (int64_t)16 * cus / a.rows));
   a.each = (int32_t)std::max<int64_t>((n + (waves == 4 ? 3 : waves / 2)) / waves, (n + 511) / 512);
   a.splits = (n + 4 * a.each - 1) / (4 * a.each);
 }
