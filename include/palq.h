@@ -599,14 +599,23 @@ palq_status palq_rotation_create(palq_ctx *ctx, const double *freq, int32_t pair
 /* Frees a rotation (waits for device work that still reads it). */
 void palq_rotation_destroy(palq_rotation *rot);
 
+/* Queries or keys of a batch and where their results go: [tokens][heads][head_dim], strides
+ * in elements as in palq_cache_append; weight: fp32 [head_dim], or NULL for ones. */
+typedef struct {
+  const void *x;
+  int64_t row, head;
+  void *out;
+  int64_t out_row, out_head;
+  const float *weight;
+  int32_t heads;
+} palq_heads;
+
 /* RMS norm of every head of queries and keys, then the rotation of its pairs
  * (a, b) by position, in fp32 and with one rounding:
  *   y = x / sqrt(mean(x^2) + eps) * weight,  t = position * freq,
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
- * q, k and their results: `type` (PALQ_F32, F16 or BF16) [tokens][heads]
- * [head_dim], head_dim 64, 96, 128 or 256, strides in elements as in
- * palq_cache_append; q_heads or k_heads 0: no such tensor.  eps 0: no norm;
- * weights fp32 [head_dim], or NULL for ones.  rot NULL: no rotation.  Row i of
+ * q, k (either may be NULL): `type` (PALQ_F32, F16 or BF16), head_dim 64, 96, 128
+ * or 256.  eps 0: no norm, and no weights.  rot NULL: no rotation.  Row i of
  * request r is at position lens[r] - starts[r + 1] + i, or where `tree`
  * (nullable) puts it; its fraction of a turn is exact to position 2^-65 and the
  * rounding of freq, however far the position.  Of the batch, table, max_pages and
@@ -614,10 +623,8 @@ void palq_rotation_destroy(palq_rotation *rot);
  * in place (the same pointer and strides); other overlaps of a result are
  * refused, where tensors of different strides count as their whole ranges.
  * Enqueues one kernel (or more where bounds are loose), and nothing else. */
-palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq_batch *batch, const palq_tree *tree, const void *q,
-                             int64_t q_row, int64_t q_head, int32_t q_heads, void *q_out, int64_t q_out_row, int64_t q_out_head,
-                             const float *q_weight, const void *k, int64_t k_row, int64_t k_head, int32_t k_heads, void *k_out,
-                             int64_t k_out_row, int64_t k_out_head, const float *k_weight, int32_t head_dim, int32_t type, float eps);
+palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq_batch *batch, const palq_tree *tree,
+                             const palq_heads *q, const palq_heads *k, int32_t head_dim, int32_t type, float eps);
 
 /* palq_attention (causal) where a window leaves a request's first tokens
  * visible: a row at position p sees the tokens j <= p with j > p - window or

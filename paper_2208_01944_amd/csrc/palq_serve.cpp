@@ -497,10 +497,8 @@ void palq_rotation_destroy(palq_rotation *rot) {
   delete rot;
 }
 
-palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq_batch *batch, const palq_tree *tree, const void *q,
-                             int64_t q_row, int64_t q_head, int32_t q_heads, void *q_out, int64_t q_out_row, int64_t q_out_head,
-                             const float *q_weight, const void *k, int64_t k_row, int64_t k_head, int32_t k_heads, void *k_out,
-                             int64_t k_out_row, int64_t k_out_head, const float *k_weight, int32_t head_dim, int32_t type, float eps) {
+palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq_batch *batch, const palq_tree *tree,
+                             const palq_heads *q, const palq_heads *k, int32_t head_dim, int32_t type, float eps) {
   if (!ctx) return PALQ_ERR_ARG;
   palq_status st;
   if (rot && rot->ctx != ctx) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: rotation of another context");
@@ -509,15 +507,24 @@ palq_status palq_norm_rotate(palq_ctx *ctx, const palq_rotation *rot, const palq
   if (head_dim != 64 && head_dim != 96 && head_dim != 128 && head_dim != 256)
     return fail(ctx, PALQ_ERR_UNSUPPORTED, "norm and rotation: head_dim not in {64,96,128,256}");
   if (rot && 2 * rot->pairs > head_dim) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: more pairs than a head has");
-  if (q_heads < 0 || k_heads < 0 || q_heads + (int64_t)k_heads < 1) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: no heads");
-  if (q_heads > 65535 || k_heads > 65535) return fail(ctx, PALQ_ERR_UNSUPPORTED, "norm and rotation: more than 65535 heads");
+  if (!q && !k) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: neither queries nor keys");
+  const palq_heads none{};
+  const palq_heads *const part[2] = {q ? q : &none, k ? k : &none};
+  if ((q && q->heads < 1) || (k && k->heads < 1)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: no heads");
+  if (part[0]->heads > 65535 || part[1]->heads > 65535)
+    return fail(ctx, PALQ_ERR_UNSUPPORTED, "norm and rotation: more than 65535 heads");
   if (!(eps == 0.0f || (eps >= FLT_MIN && eps <= FLT_MAX)))
     return fail(ctx, PALQ_ERR_ARG, "norm and rotation: eps must be 0 (no norm) or a normal positive number");
-  if (eps == 0.0f && (q_weight || k_weight)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: weights without a norm (eps 0)");
+  if (eps == 0.0f && (part[0]->weight || part[1]->weight)) return fail(ctx, PALQ_ERR_ARG, "norm and rotation: weights without a norm (eps 0)");
   const int64_t tokens = batch->tokens, size = size_of(type);
-  const Rows in[2] = {{q, q_row, q_head, q_heads}, {k, k_row, k_head, k_heads}};
-  const Rows to[2] = {{q_out, q_out_row, q_out_head, q_heads}, {k_out, k_out_row, k_out_head, k_heads}};
-  const float *weight[2] = {q_weight, k_weight};
+  Rows in[2], to[2];
+  const float *weight[2];
+  for (int i = 0; i < 2; ++i) {
+    const palq_heads &h = *part[i];
+    in[i] = Rows{h.x, h.row, h.head, h.heads};
+    to[i] = Rows{h.out, h.out_row, h.out_head, h.heads};
+    weight[i] = h.weight;
+  }
   for (int i = 0; i < 2; ++i) {
     if (in[i].heads == 0) continue;
     if ((st = check_rows(ctx, in[i].p, tokens, in[i].row, in[i].head, in[i].heads, head_dim, type)) ||

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -78,6 +79,15 @@ class BatchDesc(ctypes.Structure):
                 ("tokens", c_i64), ("max_new", c_i32), ("max_len", c_i32)]
 
 
+class HeadsDesc(ctypes.Structure):
+    _fields_ = [("x", c_p), ("row", c_i64), ("head", c_i64), ("out", c_p), ("out_row", c_i64), ("out_head", c_i64), ("weight", c_p),
+                ("heads", c_i32)]
+
+
+_pack_heads = struct.Struct("@PqqPqqPi").pack_into  # (as HeadsDesc lies in memory)
+_HEADS_SIZE = ctypes.sizeof(HeadsDesc)
+
+
 class TreeDesc(ctypes.Structure):
     _fields_ = [("mask", c_p), ("words", c_i32)]
 
@@ -142,8 +152,7 @@ _attention = _sig("palq_attention", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_
 P_TREE = ctypes.POINTER(TreeDesc)
 _rotation_create = _sig("palq_rotation_create", c_i32, c_p, ctypes.POINTER(ctypes.c_double), c_i32, c_i32, ctypes.POINTER(c_p))
 _rotation_destroy = _sig("palq_rotation_destroy", None, c_p)
-_norm_rotate = _sig("palq_norm_rotate", c_i32, c_p, c_p, P_BATCH, P_TREE, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_p, c_p, c_i64,
-                    c_i64, c_i32, c_p, c_i64, c_i64, c_p, c_i32, c_i32, c_f)
+_norm_rotate = _sig("palq_norm_rotate", c_i32, c_p, c_p, P_BATCH, P_TREE, c_p, c_p, c_i32, c_i32, c_f)
 _attention_sinks = _sig("palq_attention_sinks", c_i32, c_p, P_CACHE, P_BATCH, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32, c_f,
                         c_i32, c_i32)
 _attention_tree = _sig("palq_attention_tree", c_i32, c_p, P_CACHE, P_BATCH, P_TREE, c_p, c_i64, c_i64, c_i32, c_p, c_i64, c_i64, c_i32,
@@ -217,6 +226,8 @@ class Context:
                 stream = torch.cuda.current_stream(self.dev).cuda_stream
         else:
             self.torch = None
+        self.heads = (HeadsDesc * 2)()  # norm_rotate's descriptors, filled for each call
+        self.heads_at = [ctypes.addressof(h) for h in self.heads]
         h = c_p()
         st = _create(device, stream or 0, ctypes.byref(h))
         if st != OK:
@@ -402,8 +413,8 @@ class Context:
         if q_out.shape != shape or q1 != 1 or qo1 != 1:
             raise PalqError(ERR_ARG, "tensors must be [tokens, heads, head_dim], results of their shapes, a head's channels consecutive")
         on = d < 0 or (q.get_device() == d and q_out.get_device() == d and batch.device == d)
-        kp = ko = qw = kw = None
-        kr = kh = kn = kor = koh = 0
+        qw = kw = 0
+        keys = None
         if k is not None and k_out is not None:
             kt, kn, kd = shape = k.shape
             kr, kh, k1 = k.stride()
@@ -411,7 +422,7 @@ class Context:
             if k.dtype is not dtype or k_out.dtype is not dtype or kt != tokens or kd != dim or k_out.shape != shape or k1 != 1 or ko1 != 1:
                 raise PalqError(ERR_ARG, "k and k_out must be as q, [tokens, heads, head_dim]")
             on = on and (d < 0 or (k.get_device() == d and k_out.get_device() == d))
-            kp, ko = k.data_ptr(), k_out.data_ptr()
+            keys = self.heads_at[1]
         elif k is not None or k_out is not None:
             raise PalqError(ERR_ARG, "k and k_out go together")
         if q_weight is not None:
@@ -438,8 +449,12 @@ class Context:
             tree = _tree(self, tree, tokens)
         if batch.tokens != tokens:
             batch.tokens = batch.desc.tokens = tokens
-        st = _norm_rotate(self.h, rotation, batch.ref, tree, q.data_ptr(), qr, qh, qn, q_out.data_ptr(), qor, qoh, qw, kp, kr, kh, kn, ko, kor,
-                          koh, kw, dim, kind, eps)
+        _pack_heads(self.heads, 0, q.data_ptr(), qr, qh, q_out.data_ptr(), qor, qoh, qw, qn)
+        if keys:
+            _pack_heads(self.heads, _HEADS_SIZE, k.data_ptr(), kr, kh, k_out.data_ptr(), kor, koh, kw, kn)
+        elif kw:
+            raise PalqError(ERR_ARG, "k_weight without k")
+        st = _norm_rotate(self.h, rotation, batch.ref, tree, self.heads_at[0], keys, dim, kind, eps)
         if st:
             self._check(st)
 

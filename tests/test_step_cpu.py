@@ -43,9 +43,11 @@ def test_rotation_refusals(P, vctx):  # noqa: F811
 def rotate(P, vctx):  # noqa: F811
     """The call with good tensors: queries of 4 heads and keys of 2 within rows of 8 heads, in tensors of their own."""
     def run(rot=None, b=None, t=None, q=at(8), qr=512, qh=64, qn=4, qo=at(9), qor=256, qoh=64, qw=at(10), k=at(8, 512), kr=512, kh=64, kn=2,
-            ko=at(11), kor=128, koh=64, kw=at(12), dim=64, type=P.BF16, eps=1e-6):
-        return P._norm_rotate(vctx.h, rot, ref(batch(P)) if b is None else b, t, q, qr, qh, qn, qo, qor, qoh, qw, k, kr, kh, kn, ko, kor, koh, kw,
-                              dim, type, eps)
+            ko=at(11), kor=128, koh=64, kw=at(12), dim=64, type=P.BF16, eps=1e-6, no_q=False,
+            no_k=False):
+        h = [P.HeadsDesc(*f) for f in ((q, qr, qh, qo, qor, qoh, qw, qn), (k, kr, kh, ko, kor, koh, kw, kn))]
+        at_q, at_k = (None if none else ctypes.addressof(x) for x, none in zip(h, (no_q, no_k)))
+        return P._norm_rotate(vctx.h, rot, ref(batch(P)) if b is None else b, t, at_q, at_k, dim, type, eps)
     return run
 
 
@@ -56,11 +58,11 @@ def test_norm_rotate_refusals(P, vctx):  # noqa: F811
     other = P.Context(-1)
     _, foreign = rotation(P, other)
     assert run() == run(rot=rot) == run(t=ref(tree(P))) == P.OK
-    assert run(kn=0, k=None, ko=None) == run(qn=0, q=None, qo=None) == run(qw=None, kw=None) == run(eps=0.0, qw=None, kw=None) == P.OK
+    assert run(no_k=True) == run(no_q=True) == run(qw=None, kw=None) == run(eps=0.0, qw=None, kw=None) == run(no_k=True, k=None) == P.OK
     assert run(type=P.F32, q=at(8), k=at(8, 1024)) == P.OK
     in_place = dict(qo=at(8), qor=512, qoh=64, ko=at(8, 512), kor=512, koh=64)
     assert run(**in_place) == P.OK
-    for kw in (dict(rot=wide), dict(rot=foreign), dict(type=P.I8), dict(type=9), dict(qn=0, kn=0), dict(qn=-1), dict(eps=-1.0), dict(eps=float("nan")),
+    for kw in (dict(rot=wide), dict(rot=foreign), dict(type=P.I8), dict(type=9), dict(no_q=True, no_k=True), dict(qn=0), dict(kn=0), dict(qn=-1), dict(eps=-1.0), dict(eps=float("nan")),
                dict(eps=float("inf")), dict(eps=1e-40), dict(eps=0.0), dict(eps=0.0, qw=None), dict(q=None), dict(qo=None), dict(k=None), dict(ko=None),
                dict(q=at(8, 1)), dict(ko=at(11, 1)), dict(qw=at(10, 2)), dict(qh=63), dict(qor=63), dict(koh=32), dict(kor=-128),
                dict(qor=1 << 60), dict(qoh=64, qor=64),                            # rows of an output over each other
