@@ -78,8 +78,9 @@ def log_probs(x, scale, ids, top):
     return out, ent, top_ids, top_out, size
 
 
-def attend(cache, table, lens, starts, q, scale, window=0, sinks=0, mask=None):
-    """As oracle.serve.Cache.attend: fp64 outputs, sum p |v|, the largest |q| |k| sum, the seen tokens of each row."""
+def attend(cache, table, lens, starts, q, scale, window=0, sinks=0, mask=None, limit=None):
+    """As oracle.serve.Cache.attend: fp64 outputs, sum p |v|, the largest |q| |k| sum, the seen tokens of each row.  limit: the
+    tokens that a request holds at most; later ones are left out, and positions stay."""
     tokens, hq, dim = q.shape
     heads = cache.k.shape[1]
     group = hq // heads
@@ -89,6 +90,7 @@ def attend(cache, table, lens, starts, q, scale, window=0, sinks=0, mask=None):
     for r, ln in enumerate(lens):
         n = new_tokens(starts, r)
         old = ln - n
+        ln = ln if limit is None else min(ln, limit)
         j = np.arange(ln)
         for h in range(heads):
             k, there = cache.values(table, r, ln, h, "k")

@@ -69,12 +69,19 @@ struct TileOrder {
   int count, sink, gap;
   constexpr int at(int i) const { return i < sink ? i : i + gap; }
 };
+// Of an empty range (hi <= lo) only the tiles before lo's: tiles_seen is for those.
 constexpr TileOrder tile_order(int lo, int hi, int sinks) {
   if (hi <= 0) return {0, 0, 0};
   const int seen = sinks < hi ? sinks : hi, tiles = seen / 64 + (seen % 64 > 0), tile0 = lo >> 6;
   const int sink = tiles < tile0 ? tiles : tile0;
   if (hi <= lo) return {sink, sink, 0};
   return {sink + (hi + 63) / 64 - tile0, sink, tile0 - sink};
+}
+// The same for any rows: where the range is empty (a window that begins behind the last token that is there) nothing
+// of it brings the tile of lo, so the first tokens are the range.
+constexpr TileOrder tiles_seen(int lo, int hi, int sinks) {
+  const int seen = sinks < hi ? sinks : hi;
+  return hi <= lo && seen > 0 ? tile_order(0, seen, 0) : tile_order(lo, hi, sinks);
 }
 
 }  // namespace palq

@@ -172,7 +172,7 @@ __device__ __forceinline__ uint32_t seen16(const AttendArgs &a, const Request &q
   return m;
 }
 
-// The tiles of 64 tokens that a block of rows takes, by number: RANGE: their places; else tile_order's.
+// The tiles of 64 tokens that a block of rows takes, by number: RANGE: their places; else tiles_seen's.
 template <int SEES>
 struct Tiles {
   int first, count;
@@ -182,7 +182,7 @@ struct Tiles {
       first = lo >> 6;
       count = hi > lo ? ((hi + 63) >> 6) - first : 0;
     } else {
-      order = tile_order(lo, hi, a.sinks);
+      order = tiles_seen(lo, hi, a.sinks);
       first = 0;
       count = order.count;
     }
