@@ -615,8 +615,8 @@ typedef struct {
  *   y = x / sqrt(mean(x^2) + eps) * weight,  t = position * freq,
  *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
  * q, k (either may be NULL): `type` (PALQ_F32, F16 or BF16), head_dim 64, 96, 128
- * or 256.  eps 0: no norm, and no weights.  rot NULL: no rotation.  Row i of
- * request r is at position lens[r] - starts[r + 1] + i, or where `tree`
+ * or 256.  eps 0: no norm, and no weights; else a normal number.  rot NULL: no
+ * rotation.  Row i of request r is at position lens[r] - starts[r + 1] + i, or where `tree`
  * (nullable) puts it; its fraction of a turn is exact to position 2^-65 and the
  * rounding of freq, however far the position.  Of the batch, table, max_pages and
  * max_len have no effect.  Rows past max_new stay as they are.  Results may be

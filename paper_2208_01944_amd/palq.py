@@ -35,6 +35,7 @@ NET_KEEP_ALL, NET_TIMING, NET_GRAPH, NET_PIXEL_LAYOUT = 1, 2, 4, 8
 LAYOUT_PIXEL, LAYOUT_GROUP = 0, 1
 F32, F16, BF16, I8 = 0, 1, 2, 3  # element types of the transformer operators
 _INT_MAX = (1 << 31) - 1
+_F32_MIN = 2.0 ** -126  # the smallest normal number
 _F32, _I32 = torch.float32, torch.int32
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
 
@@ -439,8 +440,8 @@ class Context:
             raise PalqError(ERR_ARG, f"tensors or batch are not on the context's device, cuda:{d}")
         if eps is None:
             eps = 0.0
-        elif not eps > 0:
-            raise PalqError(ERR_ARG, "eps must be above 0 (None: no norm)")
+        elif not eps >= _F32_MIN:  # (as fp32 it would be 0, which means no norm, or lose bits)
+            raise PalqError(ERR_ARG, "eps must be a normal positive fp32 number (None: no norm)")
         if rotation is not None:
             if rotation.ctx is not self:
                 raise PalqError(ERR_ARG, "rotation of another context")
