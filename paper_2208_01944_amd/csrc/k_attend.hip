@@ -1160,6 +1160,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 // 25: 33.5, 37.9); heads of 256 have registers for four.
 constexpr int rows_waves(int dim, int sees) { return sees != RANGE && dim < 256 ? 8 : 4; }
 
+// Tokens that a request has rows for at most.  (max_new itself counts from the request's start, which may lie before the
+// first row.)
+int64_t most_new(const AttendArgs &a) { return std::min<int64_t>(a.b.max_new, a.b.tokens); }
+
 // Rows of a workgroup: 16 or 32 on attend_rows_kernel, 128 on attend_tile_kernel.
 // While the small blocks are at most 3 for each CU, their many waves over the
 // tokens end sooner than the tile kernel's long chain of steps, although each
@@ -1169,7 +1173,7 @@ constexpr int rows_waves(int dim, int sees) { return sees != RANGE && dim < 256 
 // or more (4 / 8 / 12 drafts of 64 behind 8000 to 16000: 99 / 191 / 279 us, 114 / 207 / 296 in small
 // blocks; behind 1000 to 2000 64 / 67 / 67, 26 / 46 / 67).
 int block_rows(const AttendArgs &a, int cus) {
-  const int64_t rows = (int64_t)a.b.max_new * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
+  const int64_t rows = most_new(a) * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
   const int64_t blocks = (rows + small - 1) / small * a.c.heads * a.b.requests;
   if (a.tree.mask && a.window == 0 && a.b.max_len >= 8192 && (rows + 127) / 128 * 128 * 8 <= rows * 9 && blocks >= cus) return 128;
   return blocks <= 3 * cus ? (int)small : 128;
@@ -1177,7 +1181,7 @@ int block_rows(const AttendArgs &a, int cus) {
 
 template <class T, int D, int SEES>
 hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
+  const int64_t rows = most_new(a) * a.group, rt = (rows + a.block - 1) / a.block;
   if (a.block == 128) {
     // one launch, unless loose bounds make it too large: then the last rows' first
     const int64_t each = (int64_t)a.splits * a.c.heads * a.b.requests, most = kMaxGroups / each;
@@ -1195,7 +1199,7 @@ hipError_t launch_attend_d(const AttendArgs &a, hipStream_t s) {
     else if constexpr (D < 256) attend_rows_kernel<T, D, 2, SEES, W><<<g, 64 * W, 0, s>>>(a);
   }
   if (a.splits > 1) {
-    const int64_t per = 256 / (D / 4), n = (int64_t)a.b.max_new * a.c.heads * a.group;
+    const int64_t per = 256 / (D / 4), n = most_new(a) * a.c.heads * a.group;
     attend_join_kernel<T, D, SEES><<<dim3((unsigned)((n + per - 1) / per), (unsigned)a.b.requests), 256, 0, s>>>(a);
   }
   return hipGetLastError();
@@ -1219,7 +1223,7 @@ hipError_t launch_attend_s(const AttendArgs &a, hipStream_t s) {
 
 bool attend_plan(AttendArgs &a, int cus) {
   a.block = block_rows(a, cus);
-  const int64_t rows = (int64_t)a.b.max_new * a.group, rt = (rows + a.block - 1) / a.block;
+  const int64_t rows = most_new(a) * a.group, rt = (rows + a.block - 1) / a.block;
   const int64_t base = std::max<int64_t>(1, rt * a.c.heads * a.b.requests);
   // Parts of a request's tokens, until two workgroups stand on every CU (one of 32
   // rows: its waves hold twice the accumulators; 4 requests, 5 tokens, window 8191: 24 us
@@ -1228,7 +1232,7 @@ bool attend_plan(AttendArgs &a, int cus) {
   const int64_t most = a.b.max_len <= 1024 ? 1 : (a.b.max_len + 511) / 512, want = (a.block == 32 ? 1 : 2) * cus;
   a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), want / base));
   if (a.sinks || a.tree.mask) {
-    const int64_t len = a.window > 0 ? std::min<int64_t>(a.b.max_len, (int64_t)a.window + (a.tree.mask ? 64 * a.tree.words : a.b.max_new) + a.sinks + 128) : a.b.max_len;
+    const int64_t len = a.window > 0 ? std::min<int64_t>(a.b.max_len, (int64_t)a.window + (a.tree.mask ? 64 * a.tree.words : most_new(a)) + a.sinks + 128) : a.b.max_len;
     // Parts of `chunk` tiles: a request has as many as it has tokens for, so that long ones do not go on alone (16 drafts
     // of 64 behind 1000 to 16384 tokens: 237 us in up to 6 parts, 267 in 4, 311 in 2), a part two tiles or more for each wave.
     // Small blocks stand one on a CU, and joining costs what a second would gain (32 of a window of 4096: 55 us in one

@@ -247,7 +247,6 @@ palq_status attend(palq_ctx *ctx, const palq_cache *cache, const palq_batch *bat
   hipSetDevice(ctx->device);
   AttendArgs a{view_of(cache), view_of(cache, batch), (const uint16_t *)q, (uint16_t *)out, q_row, q_head, out_row, out_head,
                group, causal, window, scale, 0, 1, nullptr, window > 0 ? sinks : 0, view_of(tree)};
-  if (a.b.max_new > batch->tokens) a.b.max_new = (int32_t)batch->tokens;
   if (!attend_plan(a, ctx->cus)) return fail(ctx, PALQ_ERR_UNSUPPORTED, "attention: 2^24 or more pairs of a request and a cache head");
   if (const size_t need = attend_work_bytes(a)) {
     a.part = (float *)workspace(ctx, need);
