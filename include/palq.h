@@ -617,8 +617,8 @@ typedef struct {
  * q, k (either may be NULL): `type` (PALQ_F32, F16 or BF16), head_dim 64, 96, 128
  * or 256.  eps 0: no norm, and no weights; else a normal number.  rot NULL: no
  * rotation.  Row i of request r is at position lens[r] - starts[r + 1] + i, or where `tree`
- * (nullable) puts it; its fraction of a turn is exact to position 2^-65 and the
- * rounding of freq, however far the position.  Of the batch, table, max_pages and
+ * (nullable) puts it; its fraction of a turn is that of position * freq, freq as given,
+ * to position 2^-65, however far the position.  Of the batch, table, max_pages and
  * max_len have no effect.  Rows past max_new stay as they are.  Results may be
  * in place (the same pointer and strides); other overlaps of a result are
  * refused, where tensors of different strides count as their whole ranges.

@@ -12,6 +12,7 @@
 #include "palq_internal.h"
 #include "rotate.h"
 #include "score.h"
+#include "turns.h"
 
 using namespace palq;
 
@@ -457,11 +458,7 @@ palq_status palq_rotation_create(palq_ctx *ctx, const double *freq, int32_t pair
   uint64_t phase[128];
   for (int i = 0; i < pairs; ++i) {
     if (!isfinite(freq[i])) return fail(ctx, PALQ_ERR_ARG, "rotation: a frequency is not finite");
-    // turns a position, its whole turns left out; 80-bit arithmetic, so that the rounding is below that of `freq` itself
-    long double f = (long double)freq[i] / 6.283185307179586476925286766559005768L;
-    f -= floorl(f);
-    const long double u = f * 18446744073709551616.0L;
-    phase[i] = u >= 18446744073709551615.0L ? 0 : (uint64_t)(u + 0.5L);
+    phase[i] = turns_of(freq[i]);  // (a position, whole ones left out)
   }
   palq_rotation *r = new (std::nothrow) palq_rotation();
   if (!r) return fail(ctx, PALQ_ERR_NOMEM, "rotation: host memory");
