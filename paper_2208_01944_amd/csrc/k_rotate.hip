@@ -163,8 +163,9 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(x.v[i], x.v[i], sum);
       sum = lanes_sum<L>(there ? sum : 0.0f);
-      float inv = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, mean, a.eps));
-      if (__any(sum == INFINITY)) {  // squares past fp32's range: those of x 2^-70, beside which eps is nothing
+      const float square = __builtin_fmaf(sum, mean, a.eps);
+      float inv = __builtin_amdgcn_rsqf(square);
+      if (__any(square == INFINITY)) {  // past fp32's range: the squares of x 2^-70, and eps 2^-140
         float less = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -172,7 +173,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a, int64_t first
           less = __builtin_fmaf(z, z, less);
         }
         less = lanes_sum<L>(there ? less : 0.0f);
-        if (sum == INFINITY) inv = __builtin_amdgcn_rsqf(less * mean) * 8.470329472543003e-22f;
+        const float eps = a.eps * 8.470329472543003e-22f * 8.470329472543003e-22f;
+        if (square == INFINITY) inv = __builtin_amdgcn_rsqf(__builtin_fmaf(less, mean, eps)) * 8.470329472543003e-22f;
       }
       if (a.w[which]) {
 #pragma unroll

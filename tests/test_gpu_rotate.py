@@ -1,5 +1,5 @@
 """GPU checks of head norms with rotation against the numpy oracle: frequencies of any sign and
-size."""
+size, eps of any size."""
 import numpy as np
 import pytest
 
@@ -29,3 +29,28 @@ def test_frequencies_of_any_sign_and_size(palq, dtype, dim, pairs, interleaved):
     palq.sync()
     for got, freq in ((out, f), (back, -f)):
         check_rotated(host(got), host(x), S.positions(lens, starts), dtype, freq=freq, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("eps", [1e30, 1e38, 3.3e38])
+def test_eps_beside_squares_past_the_range(palq, dtype, dim, eps):
+    """A mean of squares and an eps that fp32 holds, or nearly, and their sum does not: neither is lost."""
+    import torch
+    say("large eps", dtype, dim, eps)
+    g = np.random.default_rng(dim)
+    x = g.standard_normal((8, 3, dim)).astype(np.float32)
+    x[0] *= 1.5e19   # squares sum to more than the range, their mean is in it
+    x[1] *= 1e20
+    x[2] = 0
+    x[2, :, 5] = 1.7e19  # one square near the range's end
+    x[3] *= 1e18
+    x[4] *= 1e30
+    x[5, 1] = 0
+    x[6, 0, 3], x[6, 2] = np.inf, 2e19
+    q = dev(x, dtype)
+    out = torch.empty_like(q)
+    palq.norm_rotate(batch_of([8], [0, 8]), q, out, eps=eps)
+    palq.sync()
+    with np.errstate(invalid="ignore"):
+        check_rotated(host(out), host(q), np.arange(8), dtype, eps=eps)
