@@ -1,5 +1,5 @@
 """GPU checks of head norms with rotation against the numpy oracle: frequencies of any sign and
-size, eps of any size."""
+size, eps of any size, weights of queries and of keys."""
 import numpy as np
 import pytest
 
@@ -54,3 +54,28 @@ def test_eps_beside_squares_past_the_range(palq, dtype, dim, eps):
     palq.sync()
     with np.errstate(invalid="ignore"):
         check_rotated(host(out), host(q), np.arange(8), dtype, eps=eps)
+
+
+@pytest.mark.parametrize("which", ["k", "q", "both"])
+@pytest.mark.parametrize("tokens", [3, 9000])
+@pytest.mark.parametrize("dtype,dim,pairs,interleaved,q_heads,k_heads", [
+    ("bf16", 64, 32, False, 18, 3), ("f32", 96, 13, False, 9, 9), ("f16", 128, 64, True, 8, 2), ("f32", 128, 60, False, 4, 11), ("bf16", 256, 128, False, 5, 2)])
+def test_weights_of_queries_and_keys(palq, dtype, dim, pairs, interleaved, q_heads, k_heads, tokens, which):
+    """Each has its own weight or none, also where a wave takes the heads of both (9000 tokens)."""
+    import torch
+    from paper_2208_01944_amd import palq as P
+    say("weights", dtype, dim, pairs, interleaved, q_heads, k_heads, tokens, which)
+    g = np.random.default_rng(dim + tokens)
+    lens, starts = [tokens + 50, 77], [0, tokens - 2, tokens]
+    f = 1e4 ** -(np.arange(pairs) / pairs)
+    part = [(dev(g.standard_normal((tokens, n, dim)), dtype), g.standard_normal(dim).astype(np.float32)) for n in (q_heads, k_heads)]
+    (q, qw), (k, kw) = part
+    qw, kw = qw if which != "k" else None, kw if which != "q" else None
+    qo, ko = torch.empty_like(q), torch.empty_like(k)
+    palq.norm_rotate(batch_of(lens, starts), q, qo, k, ko, q_weight=None if qw is None else dev(qw), k_weight=None if kw is None else dev(kw), eps=1e-6,
+                     rotation=P.Rotation(palq, f, interleaved))
+    palq.sync()
+    some = np.r_[0:min(tokens, 40), tokens - 3:tokens]  # (the oracle takes long)
+    pos = S.positions(lens, starts)[some]
+    for x, got, w in ((q, qo, qw), (k, ko, kw)):
+        check_rotated(host(got)[some], host(x)[some], pos, dtype, freq=f, interleaved=interleaved, weight=w, eps=1e-6)
