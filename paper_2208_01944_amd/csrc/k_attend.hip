@@ -234,11 +234,14 @@ __device__ __forceinline__ float other_row_max(float x) {
 }
 
 // ------------------------------------------------------------ few rows
-// NQ tiles of 16 (query, head) rows a wave, 4 waves a workgroup, each wave every
-// fourth tile of 64 tokens; the waves join in LDS, splits in attend_join_kernel.
+// NQ tiles of 16 (query, head) rows a wave, W waves a workgroup (rows_waves), each wave every
+// W-th tile of 64 tokens; the waves join in LDS, splits in attend_join_kernel.
 // Operands go from memory straight into registers, one tile ahead.  32 requests of 2047
 // to 16384 tokens, 8 heads of 128, group 4 (605 MB of codes): 117 us, 5.2 TB/s (a
-// plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 21 us.
+// plain read of memory reaches 6.1); 4 requests, 5 tokens, window 8191: 21 us.  With sinks, 32
+// single tokens of a window of 4096: 50 us, 5.2 TB/s; 8 drafts of 11 to 25 tokens, heads of 96 in groups of
+// 7, behind 4095: 31 us, where 144 of 256 CUs have rows and their SIMDs are 70 % in vector instructions,
+// 17 % in products.
 template <class T, int D, int NQ, int SEES, int W>
 __global__ __launch_bounds__(64 * W, D < 256 ? 2 : 1) void attend_rows_kernel(AttendArgs a) {
   constexpr int KS = D / 32, DT = D / 16, OLD = D + 4;
@@ -483,8 +486,8 @@ __global__ __launch_bounds__(64 * W, D < 256 ? 2 : 1) void attend_rows_kernel(At
     };
     // Sinks and trees mask the products themselves, -inf times a factor above 0 (or 1, where a chunk's
     // scales may be NaN and nothing of it is seen), so that one path without masks follows in every
-    // build, all rows together.  8 drafts of 25 tokens, heads of 96 in groups of 7, window 4095: 43 us with
-    // masks at every score, 38 so (blocks of 32 rows, no parts); 16 drafts of 64, heads of 128: 297, 254.
+    // build, all rows together.  8 drafts of 25 tokens, heads of 96 in groups of 7, window 4095: 31.3 us, 33.9 with
+    // masks at every score; 16 drafts of 64, heads of 128, in blocks of 32 rows: 269, 902 (registers go to scratch).
     auto weigh_masked = [&]() __attribute__((always_inline)) {
       float fk[NQ], un[NQ], mx[NQ];
 #pragma unroll
@@ -1156,8 +1159,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
 }
 
 // Waves of attend_rows_kernel's workgroups: eight with sinks or trees, whose rows then need fewer parts that
-// are joined through memory (one token behind 700: 7.2 us, 8.0 with four; 32 of a window of 4096: 55.4, 56.6; 8 drafts of
-// 25: 33.5, 37.9); heads of 256 have registers for four.
+// are joined through memory (one token of a window of 512: 6.8 us, 7.4 with four; 32 of a window of 4096: 50.1, 51.2; 8
+// drafts of 25: 31.4, 35.3); heads of 256 have registers for four.
 constexpr int rows_waves(int dim, int sees) { return sees != RANGE && dim < 256 ? 8 : 4; }
 
 // Tokens that a request has rows for at most.  (max_new itself counts from the request's start, which may lie before the
@@ -1170,8 +1173,8 @@ int64_t most_new(const AttendArgs &a) { return std::min<int64_t>(a.b.max_new, a.
 // block converts its codes itself: 4 requests, 8 heads, group 4, 2048 tokens, 64 /
 // 128 / 256 new ones: 29 / 39 / 72 us against 35 / 40 / 58.  Drafts whose rows fill
 // blocks of 128 go there from one small block for each CU on if they are behind 8192 tokens
-// or more (4 / 8 / 12 drafts of 64 behind 8000 to 16000: 99 / 191 / 279 us, 114 / 207 / 296 in small
-// blocks; behind 1000 to 2000 64 / 67 / 67, 26 / 46 / 67).
+// or more (4 / 8 / 12 drafts of 64 behind 8000 to 16000: 88 / 176 / 256 us, 104 / 184 / 280 in small
+// blocks; behind 1000 to 2000 61 / 64 / 64, 23 / 42 / 63).
 int block_rows(const AttendArgs &a, int cus) {
   const int64_t rows = most_new(a) * a.group, small = rows <= 16 || a.c.dim == 256 ? 16 : 32;
   const int64_t blocks = (rows + small - 1) / small * a.c.heads * a.b.requests;
@@ -1234,9 +1237,9 @@ bool attend_plan(AttendArgs &a, int cus) {
   if (a.sinks || a.tree.mask) {
     const int64_t len = a.window > 0 ? std::min<int64_t>(a.b.max_len, (int64_t)a.window + (a.tree.mask ? 64 * a.tree.words : most_new(a)) + a.sinks + 128) : a.b.max_len;
     // Parts of `chunk` tiles: a request has as many as it has tokens for, so that long ones do not go on alone (16 drafts
-    // of 64 behind 1000 to 16384 tokens: 237 us in up to 6 parts, 267 in 4, 311 in 2), a part two tiles or more for each wave.
-    // Small blocks stand one on a CU, and joining costs what a second would gain (32 of a window of 4096: 55 us in one
-    // part, 63 in two).
+    // of 64 behind 1000 to 16384 tokens: 222 us in up to 6 parts, 255 in 4, 292 in 2), a part two tiles or more for each wave.
+    // Small blocks stand one on a CU, and joining costs more than a second gains (32 of a window of 4096: 50 us in one
+    // part, 58 in two; 8 drafts of 25: 31 and 45).
     const int64_t tiles = (len + 63) / 64, least = a.block == 128 ? 32 : 2 * rows_waves(a.c.dim, SINKS);
     const int64_t parts = (a.block == 128 ? 6 : 1) * cus / base;
     a.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(parts, 64), tiles / least));

@@ -58,7 +58,7 @@ __device__ __forceinline__ float lanes_sum(float x) {
 // Channels of a lane.  HALVES: of 8 pairs, channel p with p + pairs, eight of each in a row (past the rotating
 // pairs sixteen in a row).  NEIGHBOURS: 8 pairs of 2 p with 2 p + 1, sixteen in a row.  MIXED: halves that eight
 // does not divide: sixteen in a row, each with its partner's value from LDS and its own angle (22.5 k tokens, 40 heads
-// of 128: 138 us for 60 pairs, 95 for 64 in HALVES).
+// of 128 in bf16: 128 us for 60 pairs; 64 take 91 in HALVES, 99 in NEIGHBOURS).
 enum { HALVES, NEIGHBOURS, MIXED };
 
 template <class T>

@@ -266,8 +266,8 @@ __global__ __launch_bounds__(256) void score_kernel(ScoreArgs a, int64_t first_r
   typedef typename T::raw Raw;
   constexpr int VEC = 16 / sizeof(Raw), U = STEP / (64 * VEC), kStep = STEP;
   // A long step's runs of 16 bytes whose largest passes the bound wait in a queue, with their first indices, so that
-  // the few logits that pass are looked at 64 at a time; a short step looks at each of a lane's 8 (1500 rows of 50000: 51 us,
-  // 57 so in long steps; one row: 12.3 us with the queue, 11.8).
+  // the few logits that pass are looked at 64 at a time; a short step looks at each of a lane's 8 (1500 rows of 50000: 49 us,
+  // 79 so in long steps; one row: 12.0 us with the queue, 11.9).
   constexpr bool QUEUED = TOP && STEP == kLongStep;
   __shared__ v4i queue[4][QUEUED ? 64 * U : 1];
   __shared__ int ids[4][QUEUED ? 64 * U : 1];
